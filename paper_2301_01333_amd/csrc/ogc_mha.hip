@@ -23,15 +23,8 @@
 #include <string.h>
 #include <type_traits>
 
+#include "ogc_attention.h"
 #include "ogc_mha.h"
-
-typedef int v4i __attribute__((ext_vector_type(4)));
-typedef float v4f __attribute__((ext_vector_type(4)));
-typedef float v16f __attribute__((ext_vector_type(16)));
-typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
-typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
-
-#define MHA_DEV static __device__ __forceinline__
 
 struct MhaArgs {
     const uint8_t* q;
@@ -48,27 +41,6 @@ struct MhaArgs {
     float inv_scale;   // bf16, mask in LDS: 1 / scale, and the bound its quotient is held to
     float addend_max;
 };
-
-constexpr float LOG2E = 1.44269504088896340736f;
-
-MHA_DEV void swap32(uint32_t& a, uint32_t& b) {
-    auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
-    a = r[0];
-    b = r[1];
-}
-// value of x in the other half of the wavefront (lane ^ 32)
-MHA_DEV float other_half(float x) {
-    uint32_t a = __builtin_bit_cast(uint32_t, x), b = a;
-    swap32(a, b);
-    return __builtin_bit_cast(float, (threadIdx.x & 32) ? a : b);
-}
-MHA_DEV uint32_t pack_bf16(float lo, float hi) {  // round to nearest even, two values per register
-    v2bf r = {(__bf16)lo, (__bf16)hi};
-    return __builtin_bit_cast(uint32_t, r);
-}
-
-// n / d; m = floor(2^32 / d) + 1 where that is exact for every n in use (n * d < 2^32, and d > 1), else 0
-MHA_DEV uint32_t div_magic(uint32_t n, uint32_t d, uint32_t m) { return m ? __umulhi(n, m) : n / d; }
 
 // a mask of finite values stays finite when it is scaled (-infinity is for keys beyond the sequence); NaN passes
 constexpr float MHA_F32_MAX = 3.40282347e38f, MHA_MASK_LOW = -2.3e38f;  // (the latter is finite in base 2 still)

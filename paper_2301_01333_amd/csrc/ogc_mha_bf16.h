@@ -34,34 +34,10 @@
 #ifndef OGC_MHA_BF16_H
 #define OGC_MHA_BF16_H
 
-typedef short v4s __attribute__((ext_vector_type(4)));
-typedef short v8s __attribute__((ext_vector_type(8)));
-typedef __attribute__((address_space(3))) uint8_t mha_lds_u8;
-typedef __attribute__((address_space(3))) v4i mha_lds_v4i;
-typedef __attribute__((address_space(3))) v4s mha_lds_v4s;
-typedef __attribute__((address_space(3))) v4f mha_lds_v4f;
-
 constexpr int MHA_LDS_KEYS = 4096;  // longer sequences replace half of them every 64 units
-constexpr int MHA_UNIT = 32;  // keys per unit
 constexpr int MHA_PF = 2;     // units in flight ahead of the one in use
 constexpr float MHA_ADDEND_NEAR = 1024.0f;  // addends (base-2 domain) of keys that may hold a tile's references near zero
 constexpr int MHA_READ_AHEAD = 3;  // pairs of weights between an operand's LDS read and its first matrix instruction
-
-template <int D32> struct MhaB {
-    static constexpr int D = D32 * 32, ROW = D * 2, CH = ROW / 16;  // bytes and 16-byte pieces per row
-    static constexpr int UNIT_BYTES = MHA_UNIT * ROW, SLOTS = 4;
-    static constexpr int RING = 2 * SLOTS * UNIT_BYTES;  // keys, then values
-    // Position of piece c of key row r inside the row.  A read takes the same piece of eight consecutive keys (first
-    // product) or two neighbouring pieces of four consecutive ones (second): with these the eight 16-byte pieces fall
-    // on distinct groups of four banks, for rows of 64, 128, 192 and 256 bytes.
-    static constexpr bool WIDE_ROWS = CH % 8 == 0;
-    static __device__ __forceinline__ int kswz(int r) { return WIDE_ROWS ? (r & 7) : ((r >> 1) & 3); }
-    static __device__ __forceinline__ int vswz(int r) { return WIDE_ROWS ? 2 * (r & 3) : 2 * ((r >> 1) & 1); }
-};
-
-template <int N> MHA_DEV void mha_wait_and_meet() {  // all but the N newest loads have landed, LDS accesses are done, then the workgroup meets
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
-}
 
 // D32 = head_dim / 32.  PLAIN: no mask, whole units, so no key needs an addend.  The scalar is positive.
 template <int D32, int FAST, int PLAIN, int QS> MHA_DEV void mha_stream_body(const MhaArgs& a, mha_lds_u8* lds) {

@@ -21,21 +21,6 @@
 #ifndef OGC_MHA_F32_H
 #define OGC_MHA_F32_H
 
-// Three bf16 pieces of fp32 values that add up to them exactly: the nearest bf16 value, the nearest one to what is left (a
-// subtraction without rounding), and the rest, which has 7 bits.  Elements 2 t, 2 t + 1 share a register.
-struct Pieces8 {
-    v4i p[3];
-};
-MHA_DEV uint32_t upper_halves(float x, float y) {  // of values that have no others
-    return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, y), __builtin_bit_cast(uint32_t, x), 0x07060302u);
-}
-// one piece of a pair, and what is left of it
-MHA_DEV uint32_t next_piece(float& x, float& y) {
-    const uint32_t p = pack_bf16(x, y);
-    x -= __builtin_bit_cast(float, __builtin_amdgcn_alignbyte(p, 0u, 2u));  // (p << 16, for which the compiler converts x once more)
-    y -= __builtin_bit_cast(float, p & 0xffff0000u);
-    return p;
-}
 // The largest / the smallest of m and both magnitudes.  (As a builtin the former takes the masked body for 64 channels to scratch
 // memory.  The compiler does not know what the assembly's operands must keep away from: they are loaded, never computed.)
 MHA_DEV float widest(float m, float x, float y) {
@@ -45,18 +30,6 @@ MHA_DEV float widest(float m, float x, float y) {
 MHA_DEV float least(float m, float x, float y) { return __builtin_elementwise_minimum(__builtin_elementwise_minimum(fabsf(x), fabsf(y)), m); }
 // orders magnitudes, zero above all others
 MHA_DEV uint32_t zero_last(float x) { return (__builtin_bit_cast(uint32_t, x) << 1) - 1u; }
-MHA_DEV Pieces8 split8(const v4f& a, const v4f& b) {
-    Pieces8 r;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        float x = t < 2 ? a[2 * t & 3] : b[2 * t & 3], y = t < 2 ? a[(2 * t & 3) + 1] : b[(2 * t & 3) + 1];
-        r.p[0][t] = (int)next_piece(x, y);
-        r.p[1][t] = (int)next_piece(x, y);
-        r.p[2][t] = (int)upper_halves(x, y);
-    }
-    return r;
-}
-
 template <int D32> struct MhaS {
     typedef MhaB<D32> B;  // a plane (one piece of 32 keys) has the layout of a bf16 unit: 32 rows, swizzled 16-byte pieces
     static constexpr int PLANE = B::UNIT_BYTES, BLOCK = 6 * PLANE;  // three of the keys, three of the values
