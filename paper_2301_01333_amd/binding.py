@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libogc_mlp.so (include/ogc_mlp.h): argument marshalling only.
+"""Thin ctypes binding of libogc_mlp.so (include/ogc_mlp.h, ogc_mha.h, ogc_decoder.h): argument marshalling only.
 
 Every step of the path runs in the library's HIP kernels.  PyTorch appears here only as the owner
 of device memory and streams.  There is no CPU fallback: if the shared library is missing, loading
@@ -16,6 +16,7 @@ OGC_OUT_SAME, OGC_OUT_F32 = 0, 1
 OGC_MODE_AUTO, OGC_MODE_PER_LAYER, OGC_MODE_FUSED, OGC_MODE_COOP = 0, 1, 2, 3
 OGC_LAYOUT_PLAIN, OGC_LAYOUT_BLOCKED = 0, 1
 OGC_SOFTMAX_STABLE, OGC_SOFTMAX_FAST = 0, 1
+OGC_ROPE_HALF, OGC_ROPE_INTERLEAVED = 0, 1
 OGC_OK = 0
 DTYPES = {"f32": OGC_F32, "bf16": OGC_BF16, "i8": OGC_I8, "f8": OGC_F8}
 
@@ -30,6 +31,9 @@ EXPORTS = [
     "ogc_mlp_run_clocked", "ogc_mlp_clock_words_per_launch",
     "ogc_quantize_e4m3", "ogc_dequantize_e4m3",
     "ogc_mha_validate", "ogc_mha_run", "ogc_mha_kernel_name", "ogc_mha_i8_validate", "ogc_mha_run_i8", "ogc_mha_i8_kernel_name",
+    "ogc_rope_validate", "ogc_rope_run", "ogc_kv4_validate", "ogc_kv4_cache_bytes", "ogc_kv4_write", "ogc_kv4_read",
+    "ogc_kv4_attention_validate", "ogc_kv4_attention_workspace_bytes", "ogc_kv4_attention_run",
+    "ogc_prompt_validate", "ogc_prompt_run", "ogc_prompt_kernel_name",
 ]
 OGC_ERR_TIMEOUT = -8
 
@@ -61,6 +65,35 @@ class ogc_mha_desc(ctypes.Structure):
 
 class ogc_mha_quant(ctypes.Structure):
     _fields_ = [("q_scale", ctypes.c_float), ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float), ("o_scale", ctypes.c_float)]
+
+
+class ogc_rope_desc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("tokens", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("norm", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("magnitude", ctypes.c_float), ("q_stride", ctypes.c_int64 * 2),
+                ("k_stride", ctypes.c_int64 * 2), ("qo_stride", ctypes.c_int64 * 2), ("ko_stride", ctypes.c_int64 * 2)]
+
+
+class ogc_kv4_desc(ctypes.Structure):
+    _fields_ = [("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("pages", ctypes.c_int32),
+                ("batch", ctypes.c_int32), ("table_width", ctypes.c_int32)]
+
+
+class ogc_kv4_rows(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("rows", ctypes.c_int32), ("max_rows", ctypes.c_int32), ("k_stride", ctypes.c_int64 * 2),
+                ("v_stride", ctypes.c_int64 * 2)]
+
+
+class ogc_kv4_attention_desc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("rows", ctypes.c_int32), ("max_rows", ctypes.c_int32),
+                ("max_keys", ctypes.c_int32), ("scale", ctypes.c_float), ("q_stride", ctypes.c_int64 * 2), ("o_stride", ctypes.c_int64 * 2)]
+
+
+class ogc_prompt_desc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("q_rows", ctypes.c_int32), ("k_rows", ctypes.c_int32), ("max_q", ctypes.c_int32),
+                ("max_k", ctypes.c_int32), ("scale", ctypes.c_float), ("causal", ctypes.c_int32), ("q_stride", ctypes.c_int64 * 2),
+                ("k_stride", ctypes.c_int64 * 2), ("v_stride", ctypes.c_int64 * 2), ("o_stride", ctypes.c_int64 * 2)]
 
 
 class OgcError(RuntimeError):
@@ -143,6 +176,17 @@ def lib():
         l.ogc_mha_run_i8.restype = i32
         l.ogc_mha_i8_kernel_name.argtypes = [ctypes.POINTER(ogc_mha_desc)]
         l.ogc_mha_i8_kernel_name.restype = ctypes.c_char_p
+        rope, cache, rows, asks, prompt = (ctypes.POINTER(t) for t in (ogc_rope_desc, ogc_kv4_desc, ogc_kv4_rows, ogc_kv4_attention_desc,
+                                                                       ogc_prompt_desc))
+        for name, args in (("ogc_rope_validate", [rope]), ("ogc_rope_run", [rope] + 9 * [vp]),
+                           ("ogc_kv4_validate", [cache, rows]), ("ogc_kv4_cache_bytes", [cache, ctypes.POINTER(sz)]),
+                           ("ogc_kv4_write", [cache, rows] + 7 * [vp]), ("ogc_kv4_read", [cache, rows] + 7 * [vp]),
+                           ("ogc_kv4_attention_validate", [cache, asks]),
+                           ("ogc_kv4_attention_workspace_bytes", [cache, asks, ctypes.POINTER(sz)]),
+                           ("ogc_kv4_attention_run", [cache, asks] + 8 * [vp]),
+                           ("ogc_prompt_validate", [prompt]), ("ogc_prompt_run", [prompt] + 7 * [vp])):
+            getattr(l, name).argtypes, getattr(l, name).restype = args, i32
+        l.ogc_prompt_kernel_name.argtypes, l.ogc_prompt_kernel_name.restype = [prompt], ctypes.c_char_p
         _lib = l
     return _lib
 
@@ -359,6 +403,97 @@ def ogc_mha_i8_kernel_name(desc: ogc_mha_desc) -> str:
 
 def ogc_mha_kernel_name(desc: ogc_mha_desc, has_mask: bool = True) -> str:
     r = lib().ogc_mha_kernel_name(ctypes.byref(desc), int(bool(has_mask)))
+    return r.decode() if r else ""
+
+
+# ---- a decoder's attention block (include/ogc_decoder.h); strides are (row, head), in elements
+def _two(stride):
+    return (ctypes.c_int64 * 2)(int(stride[0]), int(stride[1]))
+
+
+def rope_desc(dtype: int, tokens: int, q_heads: int, kv_heads: int, head_dim: int, rot_dim: int, layout: int, norm: int, eps: float,
+              magnitude: float, q_stride, k_stride, qo_stride, ko_stride) -> ogc_rope_desc:
+    return ogc_rope_desc(int(dtype), int(tokens), int(q_heads), int(kv_heads), int(head_dim), int(rot_dim), int(layout), int(norm),
+                         float(eps), float(magnitude), _two(q_stride), _two(k_stride), _two(qo_stride), _two(ko_stride))
+
+
+def ogc_rope_validate(desc: ogc_rope_desc) -> int:
+    return int(lib().ogc_rope_validate(desc))
+
+
+def ogc_rope_run(desc: ogc_rope_desc, q_ptr: int, k_ptr: int, q_weight_ptr: int, k_weight_ptr: int, positions_ptr: int,
+                 frequencies_ptr: int, q_out_ptr: int, k_out_ptr: int, stream: int = 0) -> None:
+    _check(lib().ogc_rope_run(desc, q_ptr, k_ptr, q_weight_ptr, k_weight_ptr, positions_ptr, frequencies_ptr, q_out_ptr, k_out_ptr,
+                              stream), "ogc_rope_run")
+
+
+def kv4_desc(kv_heads: int, head_dim: int, page_size: int, pages: int, batch: int, table_width: int) -> ogc_kv4_desc:
+    return ogc_kv4_desc(int(kv_heads), int(head_dim), int(page_size), int(pages), int(batch), int(table_width))
+
+
+def kv4_rows(dtype: int, rows: int, max_rows: int, k_stride, v_stride) -> ogc_kv4_rows:
+    return ogc_kv4_rows(int(dtype), int(rows), int(max_rows), _two(k_stride), _two(v_stride))
+
+
+def ogc_kv4_validate(cache: ogc_kv4_desc, rows: ogc_kv4_rows) -> int:
+    return int(lib().ogc_kv4_validate(cache, rows))
+
+
+def ogc_kv4_cache_bytes(cache: ogc_kv4_desc) -> int:
+    v = ctypes.c_size_t()
+    _check(lib().ogc_kv4_cache_bytes(cache, ctypes.byref(v)), "ogc_kv4_cache_bytes")
+    return v.value
+
+
+def ogc_kv4_write(cache: ogc_kv4_desc, rows: ogc_kv4_rows, k_ptr: int, v_ptr: int, cu_ptr: int, start_ptr: int, table_ptr: int,
+                  cache_ptr: int, stream: int = 0) -> None:
+    _check(lib().ogc_kv4_write(cache, rows, k_ptr, v_ptr, cu_ptr, start_ptr, table_ptr, cache_ptr, stream), "ogc_kv4_write")
+
+
+def ogc_kv4_read(cache: ogc_kv4_desc, rows: ogc_kv4_rows, cache_ptr: int, cu_ptr: int, start_ptr: int, table_ptr: int, k_ptr: int,
+                 v_ptr: int, stream: int = 0) -> None:
+    _check(lib().ogc_kv4_read(cache, rows, cache_ptr, cu_ptr, start_ptr, table_ptr, k_ptr, v_ptr, stream), "ogc_kv4_read")
+
+
+def kv4_attention_desc(dtype: int, q_heads: int, rows: int, max_rows: int, max_keys: int, scale: float, q_stride,
+                       o_stride) -> ogc_kv4_attention_desc:
+    return ogc_kv4_attention_desc(int(dtype), int(q_heads), int(rows), int(max_rows), int(max_keys), float(scale), _two(q_stride),
+                                  _two(o_stride))
+
+
+def ogc_kv4_attention_validate(cache: ogc_kv4_desc, desc: ogc_kv4_attention_desc) -> int:
+    return int(lib().ogc_kv4_attention_validate(cache, desc))
+
+
+def ogc_kv4_attention_workspace_bytes(cache: ogc_kv4_desc, desc: ogc_kv4_attention_desc) -> int:
+    v = ctypes.c_size_t()
+    _check(lib().ogc_kv4_attention_workspace_bytes(cache, desc, ctypes.byref(v)), "ogc_kv4_attention_workspace_bytes")
+    return v.value
+
+
+def ogc_kv4_attention_run(cache: ogc_kv4_desc, desc: ogc_kv4_attention_desc, q_ptr: int, cu_ptr: int, lens_ptr: int, table_ptr: int,
+                          cache_ptr: int, o_ptr: int, workspace_ptr: int, stream: int = 0) -> None:
+    _check(lib().ogc_kv4_attention_run(cache, desc, q_ptr, cu_ptr, lens_ptr, table_ptr, cache_ptr, o_ptr, workspace_ptr, stream),
+           "ogc_kv4_attention_run")
+
+
+def prompt_desc(dtype: int, batch: int, q_heads: int, kv_heads: int, head_dim: int, q_rows: int, k_rows: int, max_q: int, max_k: int,
+                scale: float, causal: int, q_stride, k_stride, v_stride, o_stride) -> ogc_prompt_desc:
+    return ogc_prompt_desc(int(dtype), int(batch), int(q_heads), int(kv_heads), int(head_dim), int(q_rows), int(k_rows), int(max_q),
+                           int(max_k), float(scale), int(causal), _two(q_stride), _two(k_stride), _two(v_stride), _two(o_stride))
+
+
+def ogc_prompt_validate(desc: ogc_prompt_desc) -> int:
+    return int(lib().ogc_prompt_validate(desc))
+
+
+def ogc_prompt_run(desc: ogc_prompt_desc, q_ptr: int, k_ptr: int, v_ptr: int, cu_q_ptr: int, cu_k_ptr: int, o_ptr: int,
+                   stream: int = 0) -> None:
+    _check(lib().ogc_prompt_run(desc, q_ptr, k_ptr, v_ptr, cu_q_ptr, cu_k_ptr, o_ptr, stream), "ogc_prompt_run")
+
+
+def ogc_prompt_kernel_name(desc: ogc_prompt_desc) -> str:
+    r = lib().ogc_prompt_kernel_name(desc)
     return r.decode() if r else ""
 
 
