@@ -6,7 +6,7 @@
 // tile reach nearly equally far (32 queries for a group of four), and any group fits.  A row sees the keys up to its limit;
 // only the last blocks of a tile hold keys that some row does not see, and only they spend instructions on it.
 //
-// Tiles are started from the end of the longest sequence to the front: the longest first.
+// The tiles that reach furthest start first.
 #include "ogc_attention.h"
 #include "ogc_decoder.h"
 
@@ -25,32 +25,114 @@ struct PromptArgs {
     long long sq[2], sk[2], sv[2], so[2];  // bytes: row, head
     int q_rows, k_rows, max_q;
     int batch, heads, group;  // key heads, query heads of each
-    int tiles;                // of the longest sequence
     int causal;
+    int level_keys;           // keys of one of the 64 levels by which tiles are sorted
     float scale_log2;
 };
 
-// A workgroup's tile: `rows` rows of a key head of a sequence.
+// What a sequence has: its first query row and key, and how many of them.
+struct PromptSequence {
+    int q0, n, k0, m, off;  // causal: query i sees the keys up to i + off
+};
+MHA_DEV PromptSequence sequence_of(const PromptArgs& a, int b) {
+    PromptSequence s;
+    s.q0 = min(max(a.cu_q[b], 0), a.q_rows);
+    const int n = min(max(a.cu_q[b + 1], s.q0), a.q_rows) - s.q0;
+    s.n = min(n, a.max_q);
+    s.k0 = min(max(a.cu_k[b], 0), a.k_rows);
+    s.m = min(max(a.cu_k[b + 1], s.k0), a.k_rows) - s.k0;
+    s.off = s.m - n;
+    return s;
+}
+
+// A workgroup's tile: 128 rows of a key head of a sequence.
 struct PromptTile {
     int head, q0, n, m;  // key head, the sequence's first query row, its queries and keys
     int row0, off;       // first row of the tile; causal: query i sees the keys up to i + off
     const uint8_t *k, *v;
 };
-// (block ids go round the 8 XCDs: the tiles of a key head stay on one of them where there are a multiple of 8 of those)
-template <int ROWS> MHA_DEV bool tile_of(const PromptArgs& a, PromptTile& t) {
-    const uint32_t pairs = a.batch * a.heads, pair = blockIdx.x % pairs;
-    const int tile = a.tiles - 1 - (int)(blockIdx.x / pairs), b = pair / (uint32_t)a.heads;
-    t.head = pair % (uint32_t)a.heads;
-    t.q0 = min(max(a.cu_q[b], 0), a.q_rows);
-    const int n = min(max(a.cu_q[b + 1], t.q0), a.q_rows) - t.q0;
-    t.n = min(n, a.max_q);
-    const int k0 = min(max(a.cu_k[b], 0), a.k_rows);
-    t.m = min(max(a.cu_k[b + 1], k0), a.k_rows) - k0;
-    t.row0 = tile * ROWS;
-    t.off = t.m - n;
-    t.k = a.k + k0 * a.sk[0] + t.head * a.sk[1];
-    t.v = a.v + k0 * a.sv[0] + t.head * a.sv[1];
-    return t.row0 < t.n * a.group;
+constexpr int PROMPT_ROWS = 128;
+
+// x added up over the lanes up to this one
+MHA_DEV int sum_to_lane(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8: within 16 lanes
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // the sums of 16 lanes into the next 16, those of 32 into the next 32
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+// Tiles of a sequence that reach key x or further (level 0: all of them).
+MHA_DEV int tiles_from(const PromptArgs& a, const PromptSequence& s, int level) {
+    const int rows = s.n * a.group, tiles = (rows + PROMPT_ROWS - 1) / PROMPT_ROWS;
+    if (level <= 0) return tiles;
+    if (level > 63) return 0;
+    const int x = level * a.level_keys;
+    if (!a.causal) return s.m - 1 >= x ? tiles : 0;
+    const int i = x - s.off;  // the first query that does
+    if (i >= s.n) return 0;
+    if (i <= 0) return tiles;
+    return tiles - i * a.group / PROMPT_ROWS;
+}
+// The tile of this workgroup.  The tiles of all sequences are handed out from the one that reaches furthest on, sorted in 64 levels, so that no
+// workgroup but the last few is without work: workgroups are dealt to the parts of the chip in turn, whether they have work or not, and
+// a grid with a place for each sequence's every possible tile left whole parts idle (8 prompts of 370 .. 4096 tokens, 32 heads over 8 of 128 channels: 595 us, so 467).
+// A lane counts the tiles of a sequence; the level and then the sequence are found from the sums.  (Heads go round the 8 XCDs: with a multiple
+// of 8 of them a head's keys and values are in one XCD's L2.)
+MHA_DEV bool tile_of(const PromptArgs& a, PromptTile& t) {
+    int j = blockIdx.x / (uint32_t)a.heads, b = 0, tile = 0;
+    t.head = blockIdx.x % (uint32_t)a.heads;
+    if (a.batch == 1) {
+        tile = tiles_from(a, sequence_of(a, 0), 0) - 1 - j;
+        if (tile < 0) return false;
+    } else {
+        const int lane = threadIdx.x & 63;
+        PromptSequence mine = {0, 0, 0, 0, 0};
+        if (lane < a.batch) mine = sequence_of(a, lane);
+        auto all_from = [&](int level) {
+            int sum = tiles_from(a, mine, level);
+            for (int b0 = 64; b0 < a.batch; b0 += 64)
+                if (b0 + lane < a.batch) sum += tiles_from(a, sequence_of(a, b0 + lane), level);
+            return __builtin_amdgcn_readlane(sum_to_lane(sum), 63);
+        };
+        if (j >= all_from(0)) return false;
+        int level = 0, above = 0;  // the highest level from which on there are more than j tiles, and those above it
+        for (int step = 32; step > 0; step /= 2) {
+            const int c = all_from(level + step);
+            if (c > j) level += step;
+            else above = c;
+        }
+        j -= above;
+        for (int b0 = 0; b0 < a.batch; b0 += 64) {
+            int high = 0, here = 0;
+            if (b0 + lane < a.batch) {
+                const PromptSequence s = b0 ? sequence_of(a, b0 + lane) : mine;
+                high = tiles_from(a, s, level + 1);
+                here = tiles_from(a, s, level) - high;
+            }
+            const int to = sum_to_lane(here);
+            const uint64_t past = __builtin_amdgcn_ballot_w64(to > j);
+            if (past) {
+                const int l = __builtin_ctzll(past), n = __builtin_amdgcn_readlane(here, l);
+                b = b0 + l;
+                const int rows = sequence_of(a, b).n * a.group;
+                tile = (rows + PROMPT_ROWS - 1) / PROMPT_ROWS - 1 - __builtin_amdgcn_readlane(high, l) - (j - (__builtin_amdgcn_readlane(to, l) - n));
+                break;
+            }
+            j -= __builtin_amdgcn_readlane(to, 63);
+        }
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+    const PromptSequence s = sequence_of(a, b);
+    t.q0 = s.q0;
+    t.n = s.n;
+    t.m = s.m;
+    t.off = s.off;
+    t.row0 = __builtin_amdgcn_readfirstlane(tile) * PROMPT_ROWS;
+    t.k = a.k + s.k0 * a.sk[0] + t.head * a.sk[1];
+    t.v = a.v + s.k0 * a.sv[0] + t.head * a.sv[1];
+    return t.row0 >= 0 && t.row0 < t.n * a.group;
 }
 // the last key that a row sees (below zero: none); rows beyond the last one are given what that one sees
 MHA_DEV int limit_of(const PromptArgs& a, const PromptTile& t, int row) {
@@ -63,17 +145,42 @@ MHA_DEV long long row_at(const PromptArgs& a, const PromptTile& t, const long lo
 }
 
 #include "ogc_prompt_staged.h"
+#include "ogc_prompt_bf16.h"
 
 template <int DT, int D32> __global__ __launch_bounds__(256, 2) void ogc_prompt_kernel(PromptArgs a) {
     __shared__ __attribute__((aligned(16))) uint8_t k_lds[PromptStaged<DT, D32>::K_BYTES];
     __shared__ __attribute__((aligned(16))) uint8_t vt_lds[PromptStaged<DT, D32>::V_BYTES];
     PromptTile t;
-    if (!tile_of<128>(a, t)) return;
+    if (!tile_of(a, t)) return;
     prompt_staged_body<DT, D32>(a, t, k_lds, vt_lds);
+}
+
+// bf16.  Wavefronts per SIMD the registers are held to: up to 64 channels fit three.
+template <int D32> __global__ __launch_bounds__(256, D32 <= 2 ? 3 : 2) void ogc_prompt_stream_kernel(PromptArgs a) {
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+    PromptTile t;
+    if (!tile_of(a, t)) return;
+    prompt_stream_body<D32>(a, t, (mha_lds_u8*)smem);
+}
+
+// The streaming body (bf16) addresses by 32 bits of byte offset from a unit's first row: wider token strides are staged.
+bool stream_case(const ogc_prompt_desc* d) {
+    const int64_t most = ((int64_t)1 << 31) / (2 * MHA_UNIT);
+    return d->dtype == OGC_BF16 && d->k_stride[0] <= most && d->v_stride[0] <= most;
+}
+
+// Tiles of a key head in all sequences, at most: each sequence may end with a partial one.
+int64_t tiles_of(const ogc_prompt_desc* d) {
+    const int64_t group = d->q_heads / d->kv_heads, most = (int64_t)(d->max_q < d->q_rows ? d->max_q : d->q_rows) * group;
+    const int64_t packed = (int64_t)d->q_rows * group / PROMPT_ROWS + d->batch, padded = (most + PROMPT_ROWS - 1) / PROMPT_ROWS * d->batch;
+    return packed < padded ? packed : padded;
 }
 
 bool strides_ok(const int64_t s[2], int elt) { return s[0] >= 0 && s[1] >= 0 && s[0] * elt % 16 == 0 && s[1] * elt % 16 == 0; }
 
+template <int D32> void launch_stream(const PromptArgs& a, dim3 grid, hipStream_t st) {
+    hipLaunchKernelGGL((ogc_prompt_stream_kernel<D32>), grid, dim3(256), MhaB<D32>::RING, st, a);  // (64 KiB at most)
+}
 template <int DT> void launch(int d32, const PromptArgs& a, dim3 grid, hipStream_t st) {
     switch (d32) {
     case 1: hipLaunchKernelGGL((ogc_prompt_kernel<DT, 1>), grid, dim3(256), 0, st, a); break;
@@ -98,7 +205,7 @@ ogc_status ogc_prompt_validate(const ogc_prompt_desc* d) {
     // rows of a sequence, keys and their limits stay below 2^31, and so does the grid
     const int64_t most = d->max_q < d->q_rows ? d->max_q : d->q_rows, group = d->q_heads / d->kv_heads;
     if (most * group > 0x7fff0000 || d->k_rows > 0x7fff0000 - most) return OGC_ERR_SHAPE;
-    if ((int64_t)d->batch * d->kv_heads > 0x7fffffff || ((most * group + 127) / 128) * d->batch * d->kv_heads > 0x7fffffff) return OGC_ERR_SHAPE;
+    if ((int64_t)d->batch * d->kv_heads > 0x7fffffff || tiles_of(d) * d->kv_heads > 0x7fffffff || d->max_k > 0x7fff0000) return OGC_ERR_SHAPE;
     if (d->dtype != OGC_F32 && d->dtype != OGC_BF16) return OGC_ERR_UNSUPPORTED;
     if (d->head_dim % 32 != 0 || d->head_dim > 128) return OGC_ERR_UNSUPPORTED;
     const int e = d->dtype == OGC_F32 ? 4 : 2;
@@ -137,15 +244,28 @@ ogc_status ogc_prompt_run(const ogc_prompt_desc* d, const void* q, const void* k
     a.group = d->q_heads / d->kv_heads;
     a.causal = d->causal;
     a.scale_log2 = d->scale * LOG2E;
-    a.tiles = (int)(((int64_t)a.max_q * a.group + 127) / 128);
-    const dim3 grid((unsigned)((int64_t)a.tiles * a.batch * a.heads));
-    if (d->dtype == OGC_F32) launch<OGC_F32>(d->head_dim / 32, a, grid, (hipStream_t)stream);
+    a.level_keys = d->max_k / 64 + 1;
+    const dim3 grid((unsigned)(tiles_of(d) * a.heads));
+    if (stream_case(d)) {
+        switch (d->head_dim / 32) {
+        case 1: launch_stream<1>(a, grid, (hipStream_t)stream); break;
+        case 2: launch_stream<2>(a, grid, (hipStream_t)stream); break;
+        case 3: launch_stream<3>(a, grid, (hipStream_t)stream); break;
+        default: launch_stream<4>(a, grid, (hipStream_t)stream); break;
+        }
+    } else if (d->dtype == OGC_F32) launch<OGC_F32>(d->head_dim / 32, a, grid, (hipStream_t)stream);
     else launch<OGC_BF16>(d->head_dim / 32, a, grid, (hipStream_t)stream);
     return hipGetLastError() == hipSuccess ? OGC_OK : OGC_ERR_DEVICE;
 }
 
 const char* ogc_prompt_kernel_name(const ogc_prompt_desc* d) {
     if (ogc_prompt_validate(d) != OGC_OK) return nullptr;
+    if (stream_case(d)) {
+        static char streams[4][48];
+        char* s = streams[d->head_dim / 32 - 1];
+        if (!s[0]) snprintf(s, 48, "ogc_prompt_stream_kernel<%d>", d->head_dim / 32);
+        return s;
+    }
     static char names[2][4][48];
     char* s = names[d->dtype == OGC_BF16][d->head_dim / 32 - 1];
     if (!s[0]) snprintf(s, 48, "ogc_prompt_kernel<%d, %d>", d->dtype, d->head_dim / 32);

@@ -477,6 +477,17 @@ def test_prompt_several_tiles(dtype, d, group):
     run_prompt(dtype, [333, 130, 257], [333, 200, 257], 2 * group, 2, d, d)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("seed", range(3))
+def test_prompt_many_sequences(dtype, seed):
+    """More sequences than a wavefront has lanes, of all lengths, with and without earlier keys: every tile is somebody's, and nobody's twice."""
+    rng = np.random.default_rng(50 + seed)
+    qs = rng.integers(0, 20, 150)
+    qs[rng.integers(0, 150, 5)] = [130, 64, 65, 200, 1]
+    ks = qs + (rng.integers(0, 40, 150) if seed else 0)
+    run_prompt(dtype, qs.tolist(), ks.tolist(), 2 * (seed + 1), 1 + seed, 32, seed, "plain", causal=int(seed < 2))
+
+
 @pytest.mark.parametrize("order", ["plain", "heads"])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_prompt_orders(dtype, order):
