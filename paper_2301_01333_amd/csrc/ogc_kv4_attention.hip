@@ -58,11 +58,22 @@ __device__ __forceinline__ StepSequence sequence_of(const StepArgs& a, int b) {
     return s;
 }
 
-template <int N> struct Dwords;
-template <> struct Dwords<1> { typedef uint32_t type; static __device__ __forceinline__ uint32_t at(type x, int) { return x; } };
-template <> struct Dwords<2> { typedef v2u type; static __device__ __forceinline__ uint32_t at(const type& x, int i) { return x[i]; } };
-template <> struct Dwords<3> { typedef v3u type; static __device__ __forceinline__ uint32_t at(const type& x, int i) { return x[i]; } };
-template <> struct Dwords<4> { typedef v4u type; static __device__ __forceinline__ uint32_t at(const type& x, int i) { return x[i]; } };
+// N dwords of LDS, aligned to what is a power of two of them
+template <int N> struct Dwords {
+    typedef uint32_t type __attribute__((ext_vector_type(N)));
+    static __device__ __forceinline__ uint32_t at(const type& x, int i) { return x[i]; }
+    static __device__ __forceinline__ type load(const uint8_t* p) { return *(const type*)p; }
+};
+template <> struct Dwords<1> {
+    typedef uint32_t type;
+    static __device__ __forceinline__ uint32_t at(type x, int) { return x; }
+    static __device__ __forceinline__ type load(const uint8_t* p) { return *(const uint32_t*)p; }
+};
+template <> struct Dwords<3> {
+    typedef v3u type;
+    static __device__ __forceinline__ uint32_t at(const type& x, int i) { return x[i]; }
+    static __device__ __forceinline__ type load(const uint8_t* p) { return (v3u){((const uint32_t*)p)[0], ((const uint32_t*)p)[1], ((const uint32_t*)p)[2]}; }
+};
 
 // eight codes as an operand, times a power of two (the exponent's bits of `scale`)
 __device__ __forceinline__ v8bf operand(uint32_t codes, float scale) {
@@ -79,30 +90,45 @@ __device__ __forceinline__ float exponent(const v2u& x, int i) {
 __device__ __forceinline__ float half_power(float x) { return __builtin_amdgcn_exp2f(0.5f * x); }
 __device__ __forceinline__ v4f mma(const v8bf& x, const v8bf& y, const v4f& z) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, z, 0, 0, 0); }
 
-template <int D32> struct Record {  // what a lane needs of a record
-    static constexpr int NS = D32 == 3 ? 3 : 1;  // its channels have one scale, or (96 channels) up to three of them
-    typename Dwords<D32>::type k[2];
-    v2u v[D32], ks[NS], vs[D32];
-    __device__ __forceinline__ void load(const uint8_t* r, int lane) {
-        constexpr int D = D32 * 32;
-        const int g = lane >> 4, m = lane & 15, t = 8 * (m / 4);
-#pragma unroll
-        for (int b = 0; b < 2; ++b) k[b] = *(const typename Dwords<D32>::type*)(r + kv4_key_at(D, t + 4 * b + m % 4, 8 * D32 * g));
-#pragma unroll
-        for (int s = 0; s < NS; ++s) ks[s] = *(const v2u*)(r + kv4_key_scale_at(D, (D32 * g + s) / 4, t));
-#pragma unroll
-        for (int c = 0; c < D32; ++c) {
-            v[c] = *(const v2u*)(r + kv4_value_at(D, g, 32 * c + m));
-            vs[c] = *(const v2u*)(r + kv4_value_scale_at(D, c, 8 * g));
+// The records of a run of tokens, one after the other, all arithmetic the same for a whole wavefront.
+struct RecordWalk {
+    typedef const __attribute__((address_space(4))) int32_t* Entries;  // (constant memory: a scalar load, which the counted ones do not wait for)
+    Entries entries;
+    const uint8_t* heads;  // the cache's first record of this head
+    int64_t page_bytes;
+    int page_records, pages, entry, at;  // at: record inside the page
+    __device__ __forceinline__ void start(const StepArgs& a, int b, int head, int d, int token) {
+        page_records = a.page_size / KV4_TOKENS;
+        page_bytes = (int64_t)a.heads * page_records * kv4_record_bytes(d);
+        heads = a.cache + (int64_t)head * page_records * kv4_record_bytes(d);
+        entries = (Entries)(uintptr_t)(a.table + (int64_t)b * a.width);
+        pages = a.pages;
+        entry = token / a.page_size;
+        at = token % a.page_size / KV4_TOKENS;
+    }
+    // the record that the walk is at (the caller has seen to it that it is one of the table's), or nullptr where there is no page; then one further
+    __device__ __forceinline__ const uint8_t* next(int d) {
+        const int page = entries[entry];
+        const uint8_t* r = page < 0 || page >= pages ? nullptr : heads + page * page_bytes + (int64_t)at * kv4_record_bytes(d);
+        if (++at == page_records) {
+            at = 0;
+            ++entry;
         }
+        return r;
     }
 };
 
+// Wavefronts on a SIMD that the registers are held to.
+constexpr int step_waves(int dt, int t, int w) { return w == 8 || dt == OGC_F32 || t == 2 ? 2 : 3; }
+constexpr int STEP_SLOTS = 3;  // records of a wavefront in LDS: the one in use and two on their way
+
 // DT: of the queries.  T: column tiles of a wavefront.  W: wavefronts, which take the records of the split in turn.
-template <int DT, int D32, int T, int W> __global__ __launch_bounds__(64 * W) void ogc_kv4_attention_kernel(StepArgs a) {
+template <int DT, int D32, int T, int W> __global__ __launch_bounds__(64 * W, step_waves(DT, T, W)) void ogc_kv4_attention_kernel(StepArgs a) {
     constexpr int D = D32 * 32, E = DT == OGC_F32 ? 4 : 2, P = DT == OGC_F32 ? 3 : 1, ROW = D + 4;
+    constexpr int BYTES = 34 * D, RING = W * STEP_SLOTS * BYTES, JOIN = W * 16 * ROW * 4;
     __shared__ float stat_lds[2][W][16 * T];
-    __shared__ __attribute__((aligned(16))) float o_lds[W][16][ROW];
+    __shared__ __attribute__((aligned(16))) uint8_t lds[RING > JOIN ? RING : JOIN];
+    float(*const o_lds)[16][ROW] = (float(*)[16][ROW])lds;
     const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int b = blockIdx.y;
@@ -112,7 +138,6 @@ template <int DT, int D32, int T, int W> __global__ __launch_bounds__(64 * W) vo
     const int k0 = split * a.chunk;  // (the host holds splits * chunk below 2^31)
     if (c0 >= s.n * a.group || (split > 0 && k0 >= s.len)) return;
     const int k1 = min(s.len, k0 + a.chunk);
-    const int32_t* const entries = a.table + (int64_t)b * a.width;
 
     // ---- queries: the second operand of the first product, in one or three bf16 pieces
     v8bf q[T][P][D32];
@@ -140,11 +165,21 @@ template <int DT, int D32, int T, int W> __global__ __launch_bounds__(64 * W) vo
     }
     const int first_limit = s.off + c0 / (uint32_t)a.group;  // of the first column: the least
 
-    // ---- the records of this wavefront, one ahead
-    auto record_at = [&](int token) -> const uint8_t* {  // (wavefront-uniform)
-        if (token >= k1) return nullptr;
-        const int64_t at = kv4_record_at(entries, a.width, a.page_size, a.pages, a.heads, D, token, head);
-        return at < 0 ? nullptr : a.cache + at;
+    // ---- the records of this wavefront: neighbours.  They go straight into LDS, two ahead of their use, by loads that hold no registers: a
+    // record is 17 lines of 256 bytes for 128 channels, and the chip needs some 50 KiB of them on their way to every compute unit.
+    const int records = (k1 - k0 + KV4_TOKENS - 1) / KV4_TOKENS, each = (records + W - 1) / W;
+    const int first = k0 + wave * each * KV4_TOKENS, end = min(k1, first + each * KV4_TOKENS);
+    const int count = max((end - first + KV4_TOKENS - 1) / KV4_TOKENS, 0);
+    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds + wave * (STEP_SLOTS * BYTES);
+    constexpr int LOADS = D32 + 1;  // of a record: 1 KiB each, and the exponents
+    const uint32_t piece = lane * 16;
+    auto issue = [&](const uint8_t* r, int slot) {
+        const uint32_t to = __builtin_amdgcn_readfirstlane(ring + slot * BYTES);
+#pragma unroll
+        for (int i = 0; i < D32; ++i)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to + i * 1024), "v"(piece), "s"(r + i * 1024) : "memory", "m0");
+        if (lane < D / 8)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to + D32 * 1024), "v"(piece), "s"(r + D32 * 1024) : "memory", "m0");
     };
     float factor = 30.0f;  // of the weights, base-2 logarithm
 again:
@@ -155,29 +190,43 @@ again:
 #pragma unroll
         for (int d = 0; d < D32; ++d) out[t][d][0] = out[t][d][1] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
     }
-    Record<D32> next;
-    const int first = k0 + wave * KV4_TOKENS;
-    const uint8_t* r = record_at(first);
-    if (r) next.load(r, lane);
-    for (int token = first; token < k1; token += W * KV4_TOKENS) {
-        const Record<D32> x = next;
-        const bool here = r != nullptr;
-        r = record_at(token + W * KV4_TOKENS);
-        if (r) next.load(r, lane);
+    RecordWalk walk;
+    walk.start(a, b, head, D, first);
+    uint32_t there = 0;  // bit i: there is a page for the record i ahead.  (Where there is none, the cache's first record is loaded: loads are counted.)
+    auto fetch = [&](int i) {
+        const uint8_t* r = walk.next(D);
+        there |= (r ? 1u : 0u) << (STEP_SLOTS - 1);
+        issue(r ? r : a.cache, i % STEP_SLOTS);
+    };
+    for (int i = 0; i < STEP_SLOTS - 1; ++i) {
+        if (i < count) fetch(i);
+        there >>= 1;
+    }
+    for (int i = 0; i < count; ++i) {
+        const int token = first + i * KV4_TOKENS;
+        // what was read of the slot that is loaded now has been read; then all but the newest loads have landed
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (i + STEP_SLOTS - 1 < count) {
+            fetch(i + STEP_SLOTS - 1);
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STEP_SLOTS - 1) * LOADS) : "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        const bool here = there & 1;
+        there >>= 1;
         if (!here) continue;
+        const uint8_t* const r = lds + wave * (STEP_SLOTS * BYTES) + i % STEP_SLOTS * BYTES;
         const bool whole = token + KV4_TOKENS - 1 <= first_limit;
 
         v4f sc[T][2];
 #pragma unroll
         for (int tile = 0; tile < 2; ++tile) {
             v8bf k[D32];
+            const int key = 8 * (col / 4) + 4 * tile + col % 4;
+            const typename Dwords<D32>::type codes = Dwords<D32>::load(r + kv4_key_at(D, key, 8 * D32 * g));
 #pragma unroll
-            for (int d = 0; d < D32; ++d) {
-                // (a lane's byte: token 8 (m / 4) + 4 tile + m % 4 of the eight in ks)
-                const v2u& ks = x.ks[Record<D32>::NS == 1 ? 0 : d];
-                const float scale = __builtin_bit_cast(float, (ks[tile] >> (8 * (col & 3)) & 255u) << 23);
-                k[d] = operand(Dwords<D32>::at(x.k[tile], d), scale);
-            }
+            for (int d = 0; d < D32; ++d)  // (a lane's channels have one scale, for 96 of them up to three)
+                k[d] = operand(Dwords<D32>::at(codes, d), __builtin_bit_cast(float, (uint32_t)r[kv4_key_scale_at(D, (D32 * g + d) / 4, key)] << 23));
 #pragma unroll
             for (int t = 0; t < T; ++t) {
                 v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -191,17 +240,30 @@ again:
                 sc[t][tile] = acc;
             }
         }
-        v8bf w[T][P][D32];
+        float e[T][8];  // scores, then weights, of this lane's eight tokens
+        v2u see[T];     // ones in the bytes of those that the column sees
 #pragma unroll
         for (int t = 0; t < T; ++t) {
-            // ---- the eight scores of this lane: tokens 8 g + j, base-2 logarithm
-            float e[8], cand = -INFINITY;
+            // ---- tokens 8 g + j
+            float cand = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                e[j] = sc[t][j >> 2][j & 3] * a.scale_log2;
-                if (!whole && token + 8 * g + j > limit[t]) e[j] = -INFINITY;
-                cand = fmaxf(cand, e[j]);
+                e[t][j] = sc[t][j >> 2][j & 3];
+                cand = fmaxf(cand, e[t][j]);
             }
+            see[t] = (v2u){~0u, ~0u};
+            if (!whole) {  // tokens that the column does not see: their scores, and the exponents of their values, whatever stands there
+                asm volatile("");  // (a branch, not forty selections in every record)
+                cand = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const bool hidden = token + 8 * g + j > limit[t];
+                    e[t][j] = hidden ? -INFINITY : e[t][j];
+                    see[t][j / 4] &= hidden ? ~(255u << (8 * (j % 4))) : ~0u;
+                    cand = fmaxf(cand, e[t][j]);
+                }
+            }
+            cand *= a.scale_log2;  // (positive)
             // The reference of the exponentials only has to be near the maximum: it moves where a block exceeds it by 2^8.
             if (__builtin_amdgcn_ballot_w64(cand > ref[t] + 8.0f) != 0) {
                 cand = fmaxf(cand, __shfl_xor(cand, 16));
@@ -216,54 +278,55 @@ again:
             }
             const float off = ref[t] == -INFINITY ? 0.0f : factor - ref[t];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(e[j] + off);
+            for (int j = 0; j < 8; ++j) e[t][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(e[t][j], a.scale_log2, off));
             if constexpr (P == 1) {  // rounded once; the sum takes what the second product multiplies
 #pragma unroll
                 for (int j = 0; j < 8; j += 2) {
-                    const uint32_t pr = pack_bf16(e[j], e[j + 1]);
+                    const uint32_t pr = pack_bf16(e[t][j], e[t][j + 1]);
                     sum[t] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, pr), (v2bf){(__bf16)1.0f, (__bf16)1.0f}, sum[t], false);
-                    e[j] = __builtin_bit_cast(float, pr << 16);
-                    e[j + 1] = __builtin_bit_cast(float, pr & 0xffff0000u);
+                    e[t][j] = __builtin_bit_cast(float, pr << 16);
+                    e[t][j + 1] = __builtin_bit_cast(float, pr & 0xffff0000u);
                 }
             } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) sum[t] += e[j];
+                for (int j = 0; j < 8; ++j) sum[t] += e[t][j];
             }
+        }
+        // ---- O^T += V^T P^T, 32 channels at a time: the weights times the scales of their values, then two instructions
 #pragma unroll
-            for (int d = 0; d < D32; ++d) {
+        for (int d = 0; d < D32; ++d) {
+            v8bf w[T][P];
+            const v2u scales = *(const v2u*)(r + kv4_value_scale_at(D, d, 8 * g)), codes = *(const v2u*)(r + kv4_value_at(D, g, 32 * d + col));
+#pragma unroll
+            for (int t = 0; t < T; ++t) {
                 float f[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    f[j] = e[j] * exponent(x.vs[d], j);
-                    if (!whole && token + 8 * g + j > limit[t]) f[j] = 0.0f;  // (whatever stands there)
-                }
+                for (int j = 0; j < 8; ++j) f[j] = e[t][j] * exponent(scales & see[t], j);
                 if constexpr (P == 1) {
                     const v4i r = {(int)upper_halves(f[0], f[1]), (int)upper_halves(f[2], f[3]), (int)upper_halves(f[4], f[5]), (int)upper_halves(f[6], f[7])};
-                    w[t][0][d] = __builtin_bit_cast(v8bf, r);
+                    w[t][0] = __builtin_bit_cast(v8bf, r);
                 } else {
                     const Pieces8 r = split8((v4f){f[0], f[1], f[2], f[3]}, (v4f){f[4], f[5], f[6], f[7]});
 #pragma unroll
-                    for (int p = 0; p < 3; ++p) w[t][p][d] = __builtin_bit_cast(v8bf, r.p[p]);
+                    for (int p = 0; p < 3; ++p) w[t][p] = __builtin_bit_cast(v8bf, r.p[p]);
                 }
             }
-        }
-#pragma unroll
-        for (int d = 0; d < D32; ++d)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const v8bf v = operand(x.v[d][h], 1.0f);
+                const v8bf v = operand(codes[h], 1.0f);
 #pragma unroll
                 for (int t = 0; t < T; ++t) {
                     if constexpr (P == 1) {
-                        out[t][d][h] = mma(v, w[t][0][d], out[t][d][h]);
+                        out[t][d][h] = mma(v, w[t][0], out[t][d][h]);
                     } else {  // a record's sum by itself, small products first
                         v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                        for (int p = 2; p >= 0; --p) acc = mma(v, w[t][p][d], acc);
+                        for (int p = 2; p >= 0; --p) acc = mma(v, w[t][p], acc);
                         out[t][d][h] += acc;
                     }
                 }
             }
+        }
     }
 
     bool finite = true;
@@ -333,22 +396,57 @@ again:
     }
 }
 
-// The splits of a query and head together: four channels a thread.
+// The splits of a query and head together: a workgroup each, four channels a thread, LANES threads for them, which take the splits in turn.
 template <int DT, int D> __global__ __launch_bounds__(256) void ogc_kv4_attention_join_kernel(StepArgs a) {
+    constexpr int CH = D / 4, LANES = D == 96 ? 8 : 256 / CH;
+    __shared__ float stat_lds[2][LANES];
+    __shared__ __attribute__((aligned(16))) float o_lds[LANES][D];
     const StepSequence s = sequence_of(a, blockIdx.y);
-    const uint32_t u = blockIdx.x * 256 + threadIdx.x, heads = a.heads * a.group;
-    const int ch = u % (D / 4) * 4, hd = u / (D / 4) % heads, i = u / (D / 4) / heads;
+    const uint32_t heads = a.heads * a.group;
+    const int ch = threadIdx.x % CH * 4, lane = threadIdx.x / CH, hd = blockIdx.x % heads, i = blockIdx.x / heads;
     if (i >= s.n) return;
     const int n = (s.len + a.chunk - 1) / a.chunk;
     const long long at = (long long)(s.row0 + i) * heads + hd, step = (long long)a.rows * heads;
     float top = -INFINITY, total = 0.0f;
-    for (int k = 0; k < n; ++k) top = fmaxf(top, a.stats[2 * (at + k * step)]);
     v4f r = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k = 0; k < n; ++k) {
-        const float m = a.stats[2 * (at + k * step)], l = a.stats[2 * (at + k * step) + 1];
-        const float h = m == -INFINITY ? 0.0f : half_power(m - top);
-        total += m == -INFINITY ? l : l * h * h;
-        r += *(const v4f*)(a.partial + (at + k * step) * D + ch) * (m == -INFINITY ? l : l * h) * (m == -INFINITY ? 1.0f : h);
+    auto add = [&](float m, float l, const v4f& x) {  // sums of zero (no page, or nothing seen) have no maximum; neither have those that are no numbers
+        const float to = fmaxf(top, m), back = top == -INFINITY ? 1.0f : half_power(top - to), h = m == -INFINITY ? 1.0f : half_power(m - to);
+        total = total * back * back + l * h * h;
+        r = r * back * back + x * (l * h) * h;
+        top = to;
+    };
+    constexpr int AHEAD = 4;  // splits on their way at a time
+    for (int k0 = lane; k0 < n && lane < LANES; k0 += AHEAD * LANES) {
+        float m[AHEAD], l[AHEAD];
+        v4f x[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const long long p = at + min(k0 + k * LANES, n - 1) * step;
+            m[k] = a.stats[2 * p];
+            l[k] = a.stats[2 * p + 1];
+            x[k] = *(const v4f*)(a.partial + p * D + ch);
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (k0 + k * LANES < n) add(m[k], l[k], x[k]);
+    }
+    if (lane < LANES) {
+        if (ch == 0) stat_lds[0][lane] = top, stat_lds[1][lane] = total;
+        *(v4f*)&o_lds[lane][ch] = r;
+    }
+    __syncthreads();
+    if (lane > 0) return;
+    // (weighted sums here, not means)
+    const float own = top;
+    for (int k = 0; k < LANES; ++k) top = fmaxf(top, stat_lds[0][k]);
+    const float mine = own == -INFINITY ? 1.0f : half_power(own - top);
+    total = total * mine * mine;
+    r = r * mine * mine;
+#pragma unroll
+    for (int k = 1; k < LANES; ++k) {
+        const float m = stat_lds[0][k], h = m == -INFINITY ? 1.0f : half_power(m - top);
+        total += stat_lds[1][k] * h * h;
+        r += *(const v4f*)&o_lds[k][ch] * h * h;
     }
     if (total != 0.0f) r *= 1.0f / total;
     uint8_t* p = a.o + (s.row0 + i) * a.so[0] + hd * a.so[1] + ch * (DT == OGC_F32 ? 4 : 2);
@@ -358,14 +456,16 @@ template <int DT, int D> __global__ __launch_bounds__(256) void ogc_kv4_attentio
 
 bool strides_ok(const int64_t s[2], int elt) { return s[0] >= 0 && s[1] >= 0 && s[0] * elt % 16 == 0 && s[1] * elt % 16 == 0; }
 
-constexpr int STEP_WAVES = 4;
+constexpr int STEP_GROUPS = 768, STEP_ALONE = 1024;
 
 struct StepShape {
-    int tiles, columns, chunk, splits;
+    int waves, tiles, columns, chunk, splits;
     size_t bytes;
 };
-// How a call is cut.  Columns: 16 or (bf16) 32 a workgroup.  Tokens: as many splits as give the chip some 2048 workgroups, of 128
-// tokens at least, which is a record for each wavefront.
+// How a call is cut.  Columns: 16 or (bf16) 32 a workgroup.  Tokens: into as many splits as give the chip 768 workgroups, the three a compute unit
+// that it holds at a time for 128 channels, of a record for each of four wavefronts at least.  (With 768 / 2048, us, batch x tokens, 32 heads over 8 of
+// 128 channels: 64 x 8192 109 / 114, 32 x up to 4001 30 / 28, 1 x 4000 14 / 12; one of 30000 with 8 x 96 18 / 24.)  Up to 1024 tokens one
+// workgroup of eight wavefronts has them all: no second launch (1 x 1000: 10.2, shared 13.5; at 4000 32, shared 13).
 StepShape shape_of(const ogc_kv4_desc* c, const ogc_kv4_attention_desc* d) {
     StepShape s;
     const int group = d->q_heads / c->kv_heads;
@@ -375,39 +475,41 @@ StepShape shape_of(const ogc_kv4_desc* c, const ogc_kv4_attention_desc* d) {
     s.columns = (int)((columns + 16 * s.tiles - 1) / (16 * s.tiles));
     if (s.columns < 1) s.columns = 1;
     const int64_t keys = (int64_t)c->table_width * c->page_size < d->max_keys ? (int64_t)c->table_width * c->page_size : d->max_keys;
-    const int64_t groups = (int64_t)c->batch * c->kv_heads * s.columns, least = STEP_WAVES * KV4_TOKENS;
-    const int64_t want = groups >= 2048 ? 1 : 2048 / groups;
+    const int64_t groups = (int64_t)c->batch * c->kv_heads * s.columns, least = 4 * KV4_TOKENS;
+    const int64_t want = groups >= STEP_GROUPS ? 1 : STEP_GROUPS / groups;
     int64_t chunk = (keys + want - 1) / want;
     chunk = (chunk + least - 1) / least * least;
     if (chunk < least) chunk = least;
+    s.waves = keys <= STEP_ALONE && chunk < keys ? 8 : 4;
+    if (s.waves == 8) chunk = keys;
     s.splits = keys > 0 ? (int)((keys + chunk - 1) / chunk) : 1;
-    s.chunk = (int)(s.splits == 1 ? 0x7fffffff / least * least : chunk);
+    s.chunk = (int)(s.splits == 1 ? 0x7fffffff / 512 * 512 : chunk);
     s.bytes = s.splits > 1 ? (size_t)s.splits * d->rows * d->q_heads * (c->head_dim + 2) * 4 : 0;
     return s;
 }
 
-template <int DT, int D32, int T> void launch_step(const StepArgs& a, int batch, hipStream_t st) {
+template <int DT, int D32, int T> void launch_step(const StepArgs& a, int waves, int batch, hipStream_t st) {
     const dim3 grid((unsigned)(a.splits * a.columns * a.heads), (unsigned)batch);
-    hipLaunchKernelGGL((ogc_kv4_attention_kernel<DT, D32, T, STEP_WAVES>), grid, dim3(64 * STEP_WAVES), 0, st, a);
+    if (waves == 8) hipLaunchKernelGGL((ogc_kv4_attention_kernel<DT, D32, T, 8>), grid, dim3(64 * 8), 0, st, a);
+    else hipLaunchKernelGGL((ogc_kv4_attention_kernel<DT, D32, T, 4>), grid, dim3(64 * 4), 0, st, a);
 }
-template <int DT, int D32> void launch(const StepArgs& a, int tiles, int batch, hipStream_t st) {
+template <int DT, int D32> void launch(const StepArgs& a, int waves, int tiles, int batch, hipStream_t st) {
     if constexpr (DT == OGC_BF16) {
-        if (tiles == 2) launch_step<DT, D32, 2>(a, batch, st);
-        else launch_step<DT, D32, 1>(a, batch, st);
+        if (tiles == 2) launch_step<DT, D32, 2>(a, waves, batch, st);
+        else launch_step<DT, D32, 1>(a, waves, batch, st);
     } else {
-        launch_step<DT, D32, 1>(a, batch, st);
+        launch_step<DT, D32, 1>(a, waves, batch, st);
     }
     if (a.splits > 1) {
-        const int64_t items = (int64_t)a.max_rows * a.heads * a.group * (D32 * 8);
-        hipLaunchKernelGGL((ogc_kv4_attention_join_kernel<DT, D32 * 32>), dim3((unsigned)((items + 255) / 256), (unsigned)batch), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((ogc_kv4_attention_join_kernel<DT, D32 * 32>), dim3((unsigned)(a.max_rows * a.heads * a.group), (unsigned)batch), dim3(256), 0, st, a);
     }
 }
-template <int DT> void launch_dim(int d32, const StepArgs& a, int tiles, int batch, hipStream_t st) {
+template <int DT> void launch_dim(int d32, const StepArgs& a, int waves, int tiles, int batch, hipStream_t st) {
     switch (d32) {
-    case 1: launch<DT, 1>(a, tiles, batch, st); break;
-    case 2: launch<DT, 2>(a, tiles, batch, st); break;
-    case 3: launch<DT, 3>(a, tiles, batch, st); break;
-    default: launch<DT, 4>(a, tiles, batch, st); break;
+    case 1: launch<DT, 1>(a, waves, tiles, batch, st); break;
+    case 2: launch<DT, 2>(a, waves, tiles, batch, st); break;
+    case 3: launch<DT, 3>(a, waves, tiles, batch, st); break;
+    default: launch<DT, 4>(a, waves, tiles, batch, st); break;
     }
 }
 
@@ -424,7 +526,7 @@ ogc_status ogc_kv4_attention_validate(const ogc_kv4_desc* c, const ogc_kv4_atten
     if (d->rows < 0 || d->max_rows < 0 || d->max_keys < 0 || d->q_heads <= 0) return OGC_ERR_SHAPE;
     if (d->q_heads % c->kv_heads != 0 || d->q_heads / c->kv_heads > 256) return OGC_ERR_SHAPE;
     const int max_rows = d->max_rows < d->rows ? d->max_rows : d->rows;
-    if ((int64_t)max_rows * d->q_heads * (c->head_dim / 4) > 0x7fffff00) return OGC_ERR_SHAPE;  // (a launch's items of a sequence)
+    if ((int64_t)max_rows * d->q_heads > 0x7fffff00) return OGC_ERR_SHAPE;
     if (d->dtype != OGC_F32 && d->dtype != OGC_BF16) return OGC_ERR_UNSUPPORTED;
     const int e = d->dtype == OGC_F32 ? 4 : 2;
     if (!strides_ok(d->q_stride, e) || !strides_ok(d->o_stride, e)) return OGC_ERR_ALIGNMENT;
@@ -478,8 +580,8 @@ ogc_status ogc_kv4_attention_run(const ogc_kv4_desc* c, const ogc_kv4_attention_
     a.columns = s.columns;
     a.scale_log2 = d->scale * LOG2E;
     if ((int64_t)s.splits * s.columns * a.heads > 0x7fffffff) return OGC_ERR_SHAPE;
-    if (d->dtype == OGC_F32) launch_dim<OGC_F32>(c->head_dim / 32, a, s.tiles, c->batch, (hipStream_t)stream);
-    else launch_dim<OGC_BF16>(c->head_dim / 32, a, s.tiles, c->batch, (hipStream_t)stream);
+    if (d->dtype == OGC_F32) launch_dim<OGC_F32>(c->head_dim / 32, a, s.waves, s.tiles, c->batch, (hipStream_t)stream);
+    else launch_dim<OGC_BF16>(c->head_dim / 32, a, s.waves, s.tiles, c->batch, (hipStream_t)stream);
     return hipGetLastError() == hipSuccess ? OGC_OK : OGC_ERR_DEVICE;
 }
 
