@@ -146,6 +146,7 @@ MHA_DEV long long row_at(const PromptArgs& a, const PromptTile& t, const long lo
 
 #include "ogc_prompt_staged.h"
 #include "ogc_prompt_bf16.h"
+#include "ogc_prompt_f32.h"
 
 template <int DT, int D32> __global__ __launch_bounds__(256, 2) void ogc_prompt_kernel(PromptArgs a) {
     __shared__ __attribute__((aligned(16))) uint8_t k_lds[PromptStaged<DT, D32>::K_BYTES];
@@ -163,6 +164,20 @@ template <int D32> __global__ __launch_bounds__(256, D32 <= 2 ? 3 : 2) void ogc_
     prompt_stream_body<D32>(a, t, (mha_lds_u8*)smem);
 }
 
+// fp32.  96 channels and more have a SIMD's registers for one wavefront (held to half of them, 96 channels reload spilled ones in every round, and
+// 128 do not fit: up to 700 tokens behind 333, 16 heads over 4, 4 sequences: 96 channels 109 us, so 93; 128: staged 155, so 114).
+template <int D32> __global__ __launch_bounds__(256, D32 <= 2 ? 2 : 1) void ogc_prompt_split_kernel(PromptArgs a) {
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+    PromptTile t;
+    if (!tile_of(a, t)) return;
+    prompt_split_body<D32>(a, t, smem);
+}
+
+// The split body (fp32) multiplies a row's number by 24 bits of stride: wider token strides are staged.
+bool split_case(const ogc_prompt_desc* d) {
+    const int64_t most = (int64_t)1 << 24;
+    return d->dtype == OGC_F32 && d->k_stride[0] * 4 < most && d->v_stride[0] * 4 < most;
+}
 // The streaming body (bf16) addresses by 32 bits of byte offset from a unit's first row: wider token strides are staged.
 bool stream_case(const ogc_prompt_desc* d) {
     const int64_t most = ((int64_t)1 << 31) / (2 * MHA_UNIT);
@@ -180,6 +195,14 @@ bool strides_ok(const int64_t s[2], int elt) { return s[0] >= 0 && s[1] >= 0 && 
 
 template <int D32> void launch_stream(const PromptArgs& a, dim3 grid, hipStream_t st) {
     hipLaunchKernelGGL((ogc_prompt_stream_kernel<D32>), grid, dim3(256), MhaB<D32>::RING, st, a);  // (64 KiB at most)
+}
+template <int D32> hipError_t launch_split(const PromptArgs& a, dim3 grid, hipStream_t st) {
+    if (PromptSplit<D32>::BYTES > 65536) {  // said at every such launch: the limit belongs to the current device
+        const hipError_t e = hipFuncSetAttribute((const void*)ogc_prompt_split_kernel<D32>, hipFuncAttributeMaxDynamicSharedMemorySize, PromptSplit<D32>::BYTES);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((ogc_prompt_split_kernel<D32>), grid, dim3(256), PromptSplit<D32>::BYTES, st, a);
+    return hipSuccess;
 }
 template <int DT> void launch(int d32, const PromptArgs& a, dim3 grid, hipStream_t st) {
     switch (d32) {
@@ -253,6 +276,10 @@ ogc_status ogc_prompt_run(const ogc_prompt_desc* d, const void* q, const void* k
         case 3: launch_stream<3>(a, grid, (hipStream_t)stream); break;
         default: launch_stream<4>(a, grid, (hipStream_t)stream); break;
         }
+    } else if (split_case(d)) {
+        const int d32 = d->head_dim / 32;
+        const hipError_t e = d32 == 1 ? launch_split<1>(a, grid, (hipStream_t)stream) : d32 == 2 ? launch_split<2>(a, grid, (hipStream_t)stream) : d32 == 3 ? launch_split<3>(a, grid, (hipStream_t)stream) : launch_split<4>(a, grid, (hipStream_t)stream);
+        if (e != hipSuccess) return OGC_ERR_DEVICE;
     } else if (d->dtype == OGC_F32) launch<OGC_F32>(d->head_dim / 32, a, grid, (hipStream_t)stream);
     else launch<OGC_BF16>(d->head_dim / 32, a, grid, (hipStream_t)stream);
     return hipGetLastError() == hipSuccess ? OGC_OK : OGC_ERR_DEVICE;
@@ -264,6 +291,12 @@ const char* ogc_prompt_kernel_name(const ogc_prompt_desc* d) {
         static char streams[4][48];
         char* s = streams[d->head_dim / 32 - 1];
         if (!s[0]) snprintf(s, 48, "ogc_prompt_stream_kernel<%d>", d->head_dim / 32);
+        return s;
+    }
+    if (split_case(d)) {
+        static char splits[4][48];
+        char* s = splits[d->head_dim / 32 - 1];
+        if (!s[0]) snprintf(s, 48, "ogc_prompt_split_kernel<%d>", d->head_dim / 32);
         return s;
     }
     static char names[2][4][48];
