@@ -13,8 +13,6 @@
 #include <stdio.h>
 #include <type_traits>
 
-namespace {
-
 struct PromptArgs {
     const uint8_t* q;
     const uint8_t* k;
@@ -173,17 +171,19 @@ template <int D32> __global__ __launch_bounds__(256, D32 <= 2 ? 2 : 1) void ogc_
     prompt_split_body<D32>(a, t, smem);
 }
 
-// The split body (fp32) multiplies a row's number by 24 bits of stride: wider token strides are staged.
-bool split_case(const ogc_prompt_desc* d) {
-    const int64_t most = (int64_t)1 << 24;
-    return d->dtype == OGC_F32 && d->k_stride[0] * 4 < most && d->v_stride[0] * 4 < most;
-}
+namespace {
+
 // The streaming body (bf16) addresses by 32 bits of byte offset from a unit's first row: wider token strides are staged.
 bool stream_case(const ogc_prompt_desc* d) {
     const int64_t most = ((int64_t)1 << 31) / (2 * MHA_UNIT);
     return d->dtype == OGC_BF16 && d->k_stride[0] <= most && d->v_stride[0] <= most;
 }
 
+// The split body (fp32) multiplies a row's number by 24 bits of stride: wider token strides are staged.
+bool split_case(const ogc_prompt_desc* d) {
+    const int64_t most = (int64_t)1 << 24;
+    return d->dtype == OGC_F32 && d->k_stride[0] * 4 < most && d->v_stride[0] * 4 < most;
+}
 // Tiles of a key head in all sequences, at most: each sequence may end with a partial one.
 int64_t tiles_of(const ogc_prompt_desc* d) {
     const int64_t group = d->q_heads / d->kv_heads, most = (int64_t)(d->max_q < d->q_rows ? d->max_q : d->q_rows) * group;

@@ -1,6 +1,9 @@
 """The decoder's attention block on the host: the cache's layout arithmetic (csrc/ogc_kv4_layout.h, compiled here) against the documented
 order, places out of range, and the refusals of every entry point (found before any launch: no device is needed)."""
+import itertools
 import os
+import re
+import shutil
 import subprocess
 
 import pytest
@@ -279,3 +282,14 @@ def test_null_descriptions_are_refused():
     assert l.ogc_kv4_cache_bytes(cache(), None) == ARG and l.ogc_kv4_attention_workspace_bytes(cache(), asks(), None) == ARG
     assert l.ogc_rope_run(None, *(9 * none)) == ARG and l.ogc_prompt_run(None, *(7 * none)) == ARG
     assert l.ogc_kv4_write(None, None, *(7 * none)) == ARG and l.ogc_kv4_attention_run(None, None, *(8 * none)) == ARG
+
+
+@built
+def test_reported_kernel_names_are_in_the_library():
+    nm = shutil.which("nm") or "/opt/rocm/llvm/bin/llvm-nm"
+    out = subprocess.run([nm, "-C", "--defined-only", b.LIB_PATH], check=True, capture_output=True, text=True).stdout
+    kernels, seen = set(re.findall(r"\bvoid (ogc_\w+<[^>]*>)\(", out)), set()
+    for dtype, d, wide in itertools.product((b.OGC_F32, b.OGC_BF16), (32, 64, 96, 128), (False, True)):
+        stride = ((1 << 26) if wide else 2 * d, d)  # (a token's stride too wide for 32 bits of offset)
+        seen.add(b.ogc_prompt_kernel_name(prompt(dtype=dtype, head_dim=d, k_stride=stride, v_stride=stride)))
+    assert len(seen) == 16 and seen <= kernels

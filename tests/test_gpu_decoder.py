@@ -604,3 +604,41 @@ def test_streams_and_graph_replays():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(outs, want)), i
+
+
+# ---- the block as a program has it ------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_decoder_block(dtype):
+    """Prompts, then single tokens, against the oracle on what the kernels before it left (each is held to its own tolerance above)."""
+    torch = torch_()
+    from paper_2301_01333_amd.decoder import DecoderAttention
+
+    hq, hk, d, lens, steps = 6, 2, 64, [70, 0, 33], 3
+    g = torch.Generator(device="cuda").manual_seed(5)
+    make = lambda n: torch.randn((n, hq + 2 * hk, d), generator=g, device="cuda").to(dt(dtype))  # noqa: E731
+    w = torch.ones(d, device="cuda")
+    block = DecoderAttention(dtype, hq, hk, d, len(lens), 80, page_size=32, q_weight=w, k_weight=w)
+    scale = float(np.float32(d ** -0.5))
+    qkv = make(sum(lens))
+    o = block.prefill(qkv, lens)
+    q, k, v = (x.double().cpu().numpy() for x in block._turned(qkv, torch.cat([torch.arange(n, dtype=torch.int32) for n in lens]).cuda()))
+    at = 0
+    for n in lens:
+        want = decoder.attend(q[at:at + n], k[at:at + n], v[at:at + n], np.tril(np.ones((n, n), dtype=bool)), scale)
+        inside(o[at:at + n], want[0], tolerance(dtype, *want, n, d), "prompt of %d" % n)
+        at += n
+    for s in range(steps):
+        qkv = make(len(lens))
+        q = block._turned(qkv, block.lens.clone())[0].double().cpu().numpy()
+        o = block.step(qkv)
+        data = decoder.Cache(block.cache.cpu().numpy().reshape(-1, hk, 1, 34 * d), hk, d, 32)
+        for b, n in enumerate(lens):
+            count = n + s + 1
+            k, v = (np.array([data.read(block.table[b].tolist(), t, which) for t in range(count)]) for which in (0, 1))
+            want = decoder.attend(q[b:b + 1], k, v, np.ones((1, count), dtype=bool), scale)
+            inside(o[b:b + 1], want[0], tolerance(dtype, *want, count, d), "step %d of sequence %d" % (s, b))
+    assert block.lens.tolist() == [n + steps for n in lens]
+    with pytest.raises(ValueError):
+        block.prefill(make(5), [5, 0])
+    with pytest.raises(ValueError):
+        block.step(make(2))
