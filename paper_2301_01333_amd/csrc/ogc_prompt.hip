@@ -43,13 +43,13 @@ MHA_DEV PromptSequence sequence_of(const PromptArgs& a, int b) {
     return s;
 }
 
-// A workgroup's tile: 128 rows of a key head of a sequence.
+// A workgroup's tile: 128 rows (few tiles: 32) of a key head of a sequence.
 struct PromptTile {
     int head, q0, n, m;  // key head, the sequence's first query row, its queries and keys
     int row0, off;       // first row of the tile; causal: query i sees the keys up to i + off
     const uint8_t *k, *v;
 };
-constexpr int PROMPT_ROWS = 128;
+constexpr int PROMPT_ROWS = 128, PROMPT_FEW = 32;
 
 // x added up over the lanes up to this one
 MHA_DEV int sum_to_lane(int x) {
@@ -62,8 +62,8 @@ MHA_DEV int sum_to_lane(int x) {
     return x;
 }
 // Tiles of a sequence that reach key x or further (level 0: all of them).
-MHA_DEV int tiles_from(const PromptArgs& a, const PromptSequence& s, int level) {
-    const int rows = s.n * a.group, tiles = (rows + PROMPT_ROWS - 1) / PROMPT_ROWS;
+template <int ROWS> MHA_DEV int tiles_from(const PromptArgs& a, const PromptSequence& s, int level) {
+    const int rows = s.n * a.group, tiles = (rows + ROWS - 1) / ROWS;
     if (level <= 0) return tiles;
     if (level > 63) return 0;
     const int x = level * a.level_keys;
@@ -71,27 +71,27 @@ MHA_DEV int tiles_from(const PromptArgs& a, const PromptSequence& s, int level) 
     const int i = x - s.off;  // the first query that does
     if (i >= s.n) return 0;
     if (i <= 0) return tiles;
-    return tiles - i * a.group / PROMPT_ROWS;
+    return tiles - i * a.group / ROWS;
 }
 // The tile of this workgroup.  The tiles of all sequences are handed out from the one that reaches furthest on, sorted in 64 levels, so that no
 // workgroup but the last few is without work: workgroups are dealt to the parts of the chip in turn, whether they have work or not, and
 // a grid with a place for each sequence's every possible tile left whole parts idle (8 prompts of 370 .. 4096 tokens, 32 heads over 8 of 128 channels: 595 us, so 467).
 // A lane counts the tiles of a sequence; the level and then the sequence are found from the sums.  (Heads go round the 8 XCDs: with a multiple
 // of 8 of them a head's keys and values are in one XCD's L2.)
-MHA_DEV bool tile_of(const PromptArgs& a, PromptTile& t) {
+template <int ROWS> MHA_DEV bool tile_of(const PromptArgs& a, PromptTile& t) {
     int j = blockIdx.x / (uint32_t)a.heads, b = 0, tile = 0;
     t.head = blockIdx.x % (uint32_t)a.heads;
     if (a.batch == 1) {
-        tile = tiles_from(a, sequence_of(a, 0), 0) - 1 - j;
+        tile = tiles_from<ROWS>(a, sequence_of(a, 0), 0) - 1 - j;
         if (tile < 0) return false;
     } else {
         const int lane = threadIdx.x & 63;
         PromptSequence mine = {0, 0, 0, 0, 0};
         if (lane < a.batch) mine = sequence_of(a, lane);
         auto all_from = [&](int level) {
-            int sum = tiles_from(a, mine, level);
+            int sum = tiles_from<ROWS>(a, mine, level);
             for (int b0 = 64; b0 < a.batch; b0 += 64)
-                if (b0 + lane < a.batch) sum += tiles_from(a, sequence_of(a, b0 + lane), level);
+                if (b0 + lane < a.batch) sum += tiles_from<ROWS>(a, sequence_of(a, b0 + lane), level);
             return __builtin_amdgcn_readlane(sum_to_lane(sum), 63);
         };
         if (j >= all_from(0)) return false;
@@ -106,8 +106,8 @@ MHA_DEV bool tile_of(const PromptArgs& a, PromptTile& t) {
             int high = 0, here = 0;
             if (b0 + lane < a.batch) {
                 const PromptSequence s = b0 ? sequence_of(a, b0 + lane) : mine;
-                high = tiles_from(a, s, level + 1);
-                here = tiles_from(a, s, level) - high;
+                high = tiles_from<ROWS>(a, s, level + 1);
+                here = tiles_from<ROWS>(a, s, level) - high;
             }
             const int to = sum_to_lane(here);
             const uint64_t past = __builtin_amdgcn_ballot_w64(to > j);
@@ -115,7 +115,7 @@ MHA_DEV bool tile_of(const PromptArgs& a, PromptTile& t) {
                 const int l = __builtin_ctzll(past), n = __builtin_amdgcn_readlane(here, l);
                 b = b0 + l;
                 const int rows = sequence_of(a, b).n * a.group;
-                tile = (rows + PROMPT_ROWS - 1) / PROMPT_ROWS - 1 - __builtin_amdgcn_readlane(high, l) - (j - (__builtin_amdgcn_readlane(to, l) - n));
+                tile = (rows + ROWS - 1) / ROWS - 1 - __builtin_amdgcn_readlane(high, l) - (j - (__builtin_amdgcn_readlane(to, l) - n));
                 break;
             }
             j -= __builtin_amdgcn_readlane(to, 63);
@@ -127,7 +127,7 @@ MHA_DEV bool tile_of(const PromptArgs& a, PromptTile& t) {
     t.n = s.n;
     t.m = s.m;
     t.off = s.off;
-    t.row0 = __builtin_amdgcn_readfirstlane(tile) * PROMPT_ROWS;
+    t.row0 = __builtin_amdgcn_readfirstlane(tile) * ROWS;
     t.k = a.k + s.k0 * a.sk[0] + t.head * a.sk[1];
     t.v = a.v + s.k0 * a.sv[0] + t.head * a.sv[1];
     return t.row0 >= 0 && t.row0 < t.n * a.group;
@@ -145,12 +145,13 @@ MHA_DEV long long row_at(const PromptArgs& a, const PromptTile& t, const long lo
 #include "ogc_prompt_staged.h"
 #include "ogc_prompt_bf16.h"
 #include "ogc_prompt_f32.h"
+#include "ogc_prompt_few.h"
 
 template <int DT, int D32> __global__ __launch_bounds__(256, 2) void ogc_prompt_kernel(PromptArgs a) {
     __shared__ __attribute__((aligned(16))) uint8_t k_lds[PromptStaged<DT, D32>::K_BYTES];
     __shared__ __attribute__((aligned(16))) uint8_t vt_lds[PromptStaged<DT, D32>::V_BYTES];
     PromptTile t;
-    if (!tile_of(a, t)) return;
+    if (!tile_of<PROMPT_ROWS>(a, t)) return;
     prompt_staged_body<DT, D32>(a, t, k_lds, vt_lds);
 }
 
@@ -158,8 +159,16 @@ template <int DT, int D32> __global__ __launch_bounds__(256, 2) void ogc_prompt_
 template <int D32> __global__ __launch_bounds__(256, D32 <= 2 ? 3 : 2) void ogc_prompt_stream_kernel(PromptArgs a) {
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     PromptTile t;
-    if (!tile_of(a, t)) return;
+    if (!tile_of<PROMPT_ROWS>(a, t)) return;
     prompt_stream_body<D32>(a, t, (mha_lds_u8*)smem);
+}
+
+// bf16, few tiles: 32 rows a workgroup, whose wavefronts share the keys
+template <int D32> __global__ __launch_bounds__(256, 1) void ogc_prompt_few_kernel(PromptArgs a) {
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[PromptFew<D32>::BYTES];
+    PromptTile t;
+    if (!tile_of<PROMPT_FEW>(a, t)) return;
+    prompt_few_body<D32>(a, t, smem);
 }
 
 // fp32.  96 channels and more have a SIMD's registers for one wavefront (held to half of them, 96 channels reload spilled ones in every round, and
@@ -167,7 +176,7 @@ template <int D32> __global__ __launch_bounds__(256, D32 <= 2 ? 3 : 2) void ogc_
 template <int D32> __global__ __launch_bounds__(256, D32 <= 2 ? 2 : 1) void ogc_prompt_split_kernel(PromptArgs a) {
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     PromptTile t;
-    if (!tile_of(a, t)) return;
+    if (!tile_of<PROMPT_ROWS>(a, t)) return;
     prompt_split_body<D32>(a, t, smem);
 }
 
@@ -185,11 +194,17 @@ bool split_case(const ogc_prompt_desc* d) {
     return d->dtype == OGC_F32 && d->k_stride[0] * 4 < most && d->v_stride[0] * 4 < most;
 }
 // Tiles of a key head in all sequences, at most: each sequence may end with a partial one.
-int64_t tiles_of(const ogc_prompt_desc* d) {
+int64_t tiles_of(const ogc_prompt_desc* d, int rows = PROMPT_ROWS) {
     const int64_t group = d->q_heads / d->kv_heads, most = (int64_t)(d->max_q < d->q_rows ? d->max_q : d->q_rows) * group;
-    const int64_t packed = (int64_t)d->q_rows * group / PROMPT_ROWS + d->batch, padded = (most + PROMPT_ROWS - 1) / PROMPT_ROWS * d->batch;
+    const int64_t packed = (int64_t)d->q_rows * group / rows + d->batch, padded = (most + rows - 1) / rows * d->batch;
     return packed < padded ? packed : padded;
 }
+
+constexpr int FEW_TILES = 256;
+// The streaming body's calls that have too few tiles of 128 rows for the 256 compute units.  Streaming / this, us, sequences x tokens, heads: 1 x 4000,
+// 1 of 128 channels 95 / 42; 4 over 1 of 128 96 / 53; 1 x 8000, 2 of 32 97 / 39; 4 of 128 187 / 166; 1 x 1000, 4 of 64 19.6 / 10.7; 4 x up to 1500, 4 of 96 34 / 27;
+// from 256 tiles on: 2 x up to 2000, 8 over 4 of 128 53 / 53; 8 x up to 1000, 8 of 128 33 / 47; 1 x 2048, 32 over 8 of 128 59 / 115.
+bool few_case(const ogc_prompt_desc* d) { return stream_case(d) && tiles_of(d) * d->kv_heads < FEW_TILES; }
 
 bool strides_ok(const int64_t s[2], int elt) { return s[0] >= 0 && s[1] >= 0 && s[0] * elt % 16 == 0 && s[1] * elt % 16 == 0; }
 
@@ -268,8 +283,16 @@ ogc_status ogc_prompt_run(const ogc_prompt_desc* d, const void* q, const void* k
     a.causal = d->causal;
     a.scale_log2 = d->scale * LOG2E;
     a.level_keys = d->max_k / 64 + 1;
-    const dim3 grid((unsigned)(tiles_of(d) * a.heads));
-    if (stream_case(d)) {
+    const bool few = few_case(d);
+    const dim3 grid((unsigned)(tiles_of(d, few ? PROMPT_FEW : PROMPT_ROWS) * a.heads));
+    if (few) {
+        switch (d->head_dim / 32) {
+        case 1: hipLaunchKernelGGL((ogc_prompt_few_kernel<1>), grid, dim3(256), 0, (hipStream_t)stream, a); break;
+        case 2: hipLaunchKernelGGL((ogc_prompt_few_kernel<2>), grid, dim3(256), 0, (hipStream_t)stream, a); break;
+        case 3: hipLaunchKernelGGL((ogc_prompt_few_kernel<3>), grid, dim3(256), 0, (hipStream_t)stream, a); break;
+        default: hipLaunchKernelGGL((ogc_prompt_few_kernel<4>), grid, dim3(256), 0, (hipStream_t)stream, a); break;
+        }
+    } else if (stream_case(d)) {
         switch (d->head_dim / 32) {
         case 1: launch_stream<1>(a, grid, (hipStream_t)stream); break;
         case 2: launch_stream<2>(a, grid, (hipStream_t)stream); break;
@@ -287,6 +310,12 @@ ogc_status ogc_prompt_run(const ogc_prompt_desc* d, const void* q, const void* k
 
 const char* ogc_prompt_kernel_name(const ogc_prompt_desc* d) {
     if (ogc_prompt_validate(d) != OGC_OK) return nullptr;
+    if (few_case(d)) {
+        static char fews[4][48];
+        char* s = fews[d->head_dim / 32 - 1];
+        if (!s[0]) snprintf(s, 48, "ogc_prompt_few_kernel<%d>", d->head_dim / 32);
+        return s;
+    }
     if (stream_case(d)) {
         static char streams[4][48];
         char* s = streams[d->head_dim / 32 - 1];

@@ -72,10 +72,53 @@ template <int DT, int D32> MHA_DEV void careful_rows(const PromptArgs& a, const 
     }
 }
 
-// The end of every body: the 32 rows from `first` on are divided by their sums and stored (after the exchange of the halves a lane has 16
-// consecutive channels of its row), and looked through for results that are not finite.
-template <int DT, int D32> MHA_DEV void store_rows(const PromptArgs& a, const PromptTile& t, int first, v16f (&oacc)[D32], float run_sum, int keys) {
+// 32 channels (from 32 d on) of 32 rows as an accumulator holds them, to the lane's row at `op` (`on`: there is one): after the exchange of
+// the halves a lane has 16 consecutive channels
+template <int DT> MHA_DEV void store_block(uint8_t* op, int d, int h, const v16f& x, bool on) {
     constexpr int E = DT == OGC_F32 ? 4 : 2;
+    if constexpr (DT == OGC_BF16) {
+        uint32_t dw[4][2];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            dw[g][0] = pack_bf16(x[4 * g], x[4 * g + 1]);
+            dw[g][1] = pack_bf16(x[4 * g + 2], x[4 * g + 3]);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            swap32(dw[0][j], dw[2][j]);
+            swap32(dw[1][j], dw[3][j]);
+        }
+        if (on) {
+            uint8_t* dst = op + (d * 32 + 16 * h) * E;
+            *(v4i*)dst = (v4i){(int)dw[0][0], (int)dw[0][1], (int)dw[2][0], (int)dw[2][1]};
+            *(v4i*)(dst + 16) = (v4i){(int)dw[1][0], (int)dw[1][1], (int)dw[3][0], (int)dw[3][1]};
+        }
+    } else {
+        uint32_t dw[4][4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float f = x[4 * g + e];
+                dw[g][e] = __builtin_bit_cast(uint32_t, f);
+            }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            swap32(dw[0][e], dw[2][e]);
+            swap32(dw[1][e], dw[3][e]);
+        }
+        if (on) {
+            uint8_t* dst = op + (d * 32 + 16 * h) * E;
+            const int order[4] = {0, 2, 1, 3};
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *(v4i*)(dst + 16 * g) = (v4i){(int)dw[order[g]][0], (int)dw[order[g]][1], (int)dw[order[g]][2], (int)dw[order[g]][3]};
+        }
+    }
+}
+
+// The end of every body: the 32 rows from `first` on are divided by their sums and stored, and looked through for results that are not finite.
+template <int DT, int D32> MHA_DEV void store_rows(const PromptArgs& a, const PromptTile& t, int first, v16f (&oacc)[D32], float run_sum, int keys) {
     const int lane = threadIdx.x & 63, h = lane >> 5, row = first + (lane & 31), rows = t.n * a.group;
     const float total = run_sum + other_half(run_sum), inv = total == 0.0f ? 0.0f : 1.0f / total;
     uint8_t* op = a.o + row_at(a, t, a.so, min(row, rows - 1));
@@ -87,45 +130,7 @@ template <int DT, int D32> MHA_DEV void store_rows(const PromptArgs& a, const Pr
             oacc[d][r] *= inv;
             finite = finite && fabsf(oacc[d][r]) < INFINITY;
         }
-        if constexpr (DT == OGC_BF16) {
-            uint32_t dw[4][2];
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                dw[g][0] = pack_bf16(oacc[d][4 * g], oacc[d][4 * g + 1]);
-                dw[g][1] = pack_bf16(oacc[d][4 * g + 2], oacc[d][4 * g + 3]);
-            }
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                swap32(dw[0][j], dw[2][j]);
-                swap32(dw[1][j], dw[3][j]);
-            }
-            if (row < rows) {
-                uint8_t* dst = op + (d * 32 + 16 * h) * E;
-                *(v4i*)dst = (v4i){(int)dw[0][0], (int)dw[0][1], (int)dw[2][0], (int)dw[2][1]};
-                *(v4i*)(dst + 16) = (v4i){(int)dw[1][0], (int)dw[1][1], (int)dw[3][0], (int)dw[3][1]};
-            }
-        } else {
-            uint32_t dw[4][4];
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float f = oacc[d][4 * g + e];
-                    dw[g][e] = __builtin_bit_cast(uint32_t, f);
-                }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                swap32(dw[0][e], dw[2][e]);
-                swap32(dw[1][e], dw[3][e]);
-            }
-            if (row < rows) {
-                uint8_t* dst = op + (d * 32 + 16 * h) * E;
-                const int order[4] = {0, 2, 1, 3};
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    *(v4i*)(dst + 16 * g) = (v4i){(int)dw[order[g]][0], (int)dw[order[g]][1], (int)dw[order[g]][2], (int)dw[order[g]][3]};
-            }
-        }
+        store_block<DT>(op, d, h, oacc[d], row < rows);
     }
     if (first < rows && __builtin_amdgcn_ballot_w64(!finite) != 0) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (stored before it is stored again)

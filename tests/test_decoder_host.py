@@ -292,4 +292,7 @@ def test_reported_kernel_names_are_in_the_library():
     for dtype, d, wide in itertools.product((b.OGC_F32, b.OGC_BF16), (32, 64, 96, 128), (False, True)):
         stride = ((1 << 26) if wide else 2 * d, d)  # (a token's stride too wide for 32 bits of offset)
         seen.add(b.ogc_prompt_kernel_name(prompt(dtype=dtype, head_dim=d, k_stride=stride, v_stride=stride)))
-    assert len(seen) == 16 and seen <= kernels
+    many = 1 << 14
+    for d in (32, 64, 96, 128):
+        seen.add(b.ogc_prompt_kernel_name(prompt(head_dim=d, q_rows=many, max_q=many, k_rows=many, max_k=many)))
+    assert len(seen) == 20 and seen <= kernels
