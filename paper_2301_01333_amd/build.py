@@ -196,9 +196,35 @@ def check_split_attention_loops(verbose: bool = True) -> None:
         print("split attention kernels checked: %d (no spills in the loop over the keys)" % checked, flush=True)
 
 
+def check_decoder_loops(verbose: bool = True) -> None:
+    """The attention kernels over the 4-bit cache and over few prompt tiles count their direct loads: one wait for all but the newest, and one for all
+    at the end.  A load of the compiler's own in the loop (a page by the vector unit, the queries waited for in every round, a spilled
+    register) would wait for the counted ones: this compiles the kernels to assembly and fails if their loop over the keys waits
+    for vector memory otherwise or touches scratch memory."""
+    import re
+
+    checked = 0
+    for source, name, many in (("ogc_kv4_attention.hip", r"\w*ogc_kv4_attention_kernelI\w*", 24), ("ogc_prompt.hip", r"\w*ogc_prompt_few_kernelI\w*", 4)):
+        text, found = _device_assembly(source), 0
+        for m in re.finditer(r"^(%s):[^\n]*\n(.*?)\n\.Lfunc_end" % name, text, re.S | re.M):
+            lines = [l.split(";")[0] for l in m.group(2).splitlines()]
+            bodies = [lines[a:b] for a, b in _loops(lines) if any("v_mfma" in l for l in lines[a:b])]
+            body = min(bodies, key=len) if bodies else []
+            waits = [l.split()[1] for l in body if "s_waitcnt" in l and "vmcnt" in l]
+            if len(waits) != 2 or "vmcnt(0)" not in waits or any("scratch_" in l for l in body):
+                raise RuntimeError("%s: its loop over the keys waits for %s" % (m.group(1), waits))
+            found += 1
+        if found != many:
+            raise RuntimeError("%s: %d kernels found in the assembly, not %d" % (source, found, many))
+        checked += found
+    if verbose:
+        print("decoder kernels checked: %d (no waits but the counted ones in the loops over the keys)" % checked, flush=True)
+
+
 if __name__ == "__main__":
     print(build_library())
     check_stream_kernel_registers()
     check_split_attention_loops()
     check_int8_attention_loops()
+    check_decoder_loops()
     sys.exit(0)
