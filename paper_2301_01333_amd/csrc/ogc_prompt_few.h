@@ -37,7 +37,7 @@ template <int D32> MHA_DEV void prompt_few_body(const PromptArgs& a, const Promp
     for (int d = 0; d < D32; ++d) oacc[d] = zero;
     float ref = -INFINITY, run_sum = 0.0f;  // run_sum: this lane's keys only
 
-    // keys, then values of unit u into slot `to`; rows beyond the last key that is seen repeat it (no row sees them)
+    // keys, then values of unit u into slot `to`; rows beyond the last key that is seen repeat it (loads are counted: all lanes load; see below)
     auto issue = [&](int u, uint32_t to) {
         const int most = S - 1 - u * MHA_UNIT;
         const uint8_t *kg = t.k + (long long)(u * MHA_UNIT) * a.sk[0], *vg = t.v + (long long)(u * MHA_UNIT) * a.sv[0];
@@ -65,6 +65,16 @@ template <int D32> MHA_DEV void prompt_few_body(const PromptArgs& a, const Promp
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
         } else {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            // Behind the last key the values are zero: their weights are, but zero times a repeated infinity would be no number.
+            if ((u + 1) * MHA_UNIT > S) {
+                int l = lane;
+                asm volatile("" : "+v"(l));  // (nothing of this is kept in registers across the loop)
+#pragma unroll
+                for (int i = 0; i < 2 * D32; ++i)
+                    if (u * MHA_UNIT + (i * 64 + l) / B::CH >= S)
+                        *(mha_lds_v4i*)(uintptr_t)(ring + slot + L::UNIT + (i * 64 + l) * 16) = (v4i){l >> 6, l >> 6, l >> 6, l >> 6};
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            }
         }
         v16f s = zero;
 #pragma unroll
