@@ -13,9 +13,10 @@
 //                                 go into the weights, for each 32 channels (a power of two: nothing is rounded by it).
 //
 // The weights carry a factor 2^30, which the division takes out again: with the smallest scales they keep all their digits.  With
-// scales from some 2^88 on they may overflow: a workgroup that finds a sum that is not finite starts again with a factor 2^-10.
-// A scale of no number (byte 255) becomes an infinity here, and what is not finite then becomes NaN: values of the cache are finite
-// otherwise, and so are their weighted means.
+// scales from some 2^80 on their sums may overflow: a workgroup that finds one that is not finite computes its share once more with a factor
+// that all its tokens cannot overflow, and takes from that what was not finite (the other channels may hold the smallest values).
+// A scale of no number (byte 255) becomes an infinity here, and what is not finite even then becomes NaN: values of the cache are finite
+// otherwise, and so are their weighted means.  Splits are joined as means, too: their sums might overflow once more.
 #include "ogc_attention.h"
 #include "ogc_decoder.h"
 #include "ogc_kv4_host.h"
@@ -182,6 +183,7 @@ template <int DT, int D32, int T, int W> __global__ __launch_bounds__(64 * W, st
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to + D32 * 1024), "v"(piece), "s"(r + D32 * 1024) : "memory", "m0");
     };
     float factor = 30.0f;  // of the weights, base-2 logarithm
+    uint32_t bad = 0;      // of this thread's outputs (see below), those that were not finite with it
 again:
 #pragma unroll
     for (int t = 0; t < T; ++t) {
@@ -329,21 +331,10 @@ again:
         }
     }
 
-    bool finite = true;
-#pragma unroll
-    for (int t = 0; t < T; ++t)
-#pragma unroll
-        for (int d = 0; d < D32; ++d)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) finite = finite && fabsf(out[t][d][h][e]) < INFINITY;
-    if (__syncthreads_or(!finite) && factor > 0.0f) {
-        factor = -10.0f;
-        goto again;
-    }
-
     // ---- the wavefronts' shares together
+    constexpr int ROUNDS = (16 * D / 4 + 64 * W - 1) / (64 * W);  // a thread has four outputs of a column tile in each
+    static_assert(4 * T * ROUNDS <= 32, "a bit of `bad` for each of them");
+    __syncthreads();  // (every wavefront is done with its records)
 #pragma unroll
     for (int t = 0; t < T; ++t) {
         sum[t] += __shfl_xor(sum[t], 16);
@@ -360,7 +351,10 @@ again:
 #pragma unroll
             for (int h = 0; h < 2; ++h) *(v4f*)&o_lds[wave][col][32 * d + 16 * h + 4 * g] = out[t][d][h];
         __syncthreads();
-        for (int u = threadIdx.x; u < 16 * D / 4; u += 64 * W) {
+#pragma unroll
+        for (int n = 0; n < ROUNDS; ++n) {
+            const int u = threadIdx.x + 64 * W * n, bit = 4 * (ROUNDS * t + n);
+            if (u >= 16 * D / 4) continue;
             const int cc = u / (D / 4), ch = u % (D / 4) * 4, c = c0 + 16 * t + cc, i = c / (uint32_t)a.group;
             if (i >= s.n) continue;
             float top = -INFINITY, total = 0.0f;
@@ -377,22 +371,47 @@ again:
             }
             const int row = s.row0 + i, hd = head * a.group + c - i * a.group;
             const float inv = 1.0f / total;
+            uint32_t write = 15;
+            if (factor > 0.0f) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) bad |= (total == 0.0f || fabsf(r[e]) < INFINITY ? 0u : 1u) << (bit + e);
+            } else {
+                write = bad >> bit & 15u;
+            }
 #pragma unroll
             for (int e = 0; e < 4; ++e) r[e] = total == 0.0f ? 0.0f : fabsf(r[e]) < INFINITY ? r[e] * inv : NAN;
             if (a.splits > 1) {  // the mean of the split, its reference and its sum without the factor
                 const long long at = ((long long)split * a.rows + row) * (a.heads * a.group) + hd;
-                *(v4f*)(a.partial + at * D + ch) = r;
-                if (ch == 0) {
+                float* p = a.partial + at * D + ch;
+                if (write == 15u) *(v4f*)p = r;
+                else
+                    for (int e = 0; e < 4; ++e)
+                        if (write >> e & 1u) p[e] = r[e];
+                if (ch == 0 && factor > 0.0f) {
                     a.stats[2 * at] = top;
-                    a.stats[2 * at + 1] = total * (factor > 0.0f ? 0x1p-30f : 0x1p10f);
+                    a.stats[2 * at + 1] = total * 0x1p-30f;
                 }
             } else {
                 uint8_t* p = a.o + (long long)row * a.so[0] + (long long)hd * a.so[1] + ch * E;
-                if constexpr (DT == OGC_F32) *(v4f*)p = r;
-                else *(v2u*)p = (v2u){pack_bf16(r[0], r[1]), pack_bf16(r[2], r[3])};
+                const v2u two = {pack_bf16(r[0], r[1]), pack_bf16(r[2], r[3])};
+                if (write == 15u) {
+                    if constexpr (DT == OGC_F32) *(v4f*)p = r;
+                    else *(v2u*)p = two;
+                } else {
+                    for (int e = 0; e < 4; ++e) {
+                        if (!(write >> e & 1u)) continue;
+                        if constexpr (DT == OGC_F32) ((float*)p)[e] = r[e];
+                        else ((uint16_t*)p)[e] = (uint16_t)(two[e / 2] >> (16 * (e % 2)));
+                    }
+                }
             }
         }
         if (t + 1 < T) __syncthreads();
+    }
+    if (factor > 0.0f && __syncthreads_or(bad != 0)) {
+        // weights up to 2^8 (the reference follows at that distance), values below 1.5 * 2^127, and all the share's tokens
+        factor = -(8.0f + (float)(32 - __builtin_clz(max(k1 - k0, 1))));
+        goto again;
     }
 }
 
@@ -408,13 +427,7 @@ template <int DT, int D> __global__ __launch_bounds__(256) void ogc_kv4_attentio
     const int n = (s.len + a.chunk - 1) / a.chunk;
     const long long at = (long long)(s.row0 + i) * heads + hd, step = (long long)a.rows * heads;
     float top = -INFINITY, total = 0.0f;
-    v4f r = {0.0f, 0.0f, 0.0f, 0.0f};
-    auto add = [&](float m, float l, const v4f& x) {  // sums of zero (no page, or nothing seen) have no maximum; neither have those that are no numbers
-        const float to = fmaxf(top, m), back = top == -INFINITY ? 1.0f : half_power(top - to), h = m == -INFINITY ? 1.0f : half_power(m - to);
-        total = total * back * back + l * h * h;
-        r = r * back * back + x * (l * h) * h;
-        top = to;
-    };
+    v4f r = {0.0f, 0.0f, 0.0f, 0.0f};  // the mean so far
     constexpr int AHEAD = 4;  // splits on their way at a time
     for (int k0 = lane; k0 < n && lane < LANES; k0 += AHEAD * LANES) {
         float m[AHEAD], l[AHEAD];
@@ -426,9 +439,26 @@ template <int DT, int D> __global__ __launch_bounds__(256) void ogc_kv4_attentio
             l[k] = a.stats[2 * p + 1];
             x[k] = *(const v4f*)(a.partial + p * D + ch);
         }
+        // (sums of zero - no page, or nothing seen - have no maximum; neither have those that are no numbers)
+        float to = top;
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k)
-            if (k0 + k * LANES < n) add(m[k], l[k], x[k]);
+        for (int k = 0; k < AHEAD; ++k) {
+            if (k0 + k * LANES >= n) m[k] = -INFINITY, l[k] = 0.0f, x[k] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+            to = fmaxf(to, m[k]);
+        }
+        const float back = top == -INFINITY ? 1.0f : half_power(top - to), before = total * back * back;
+        total = before;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const float h = m[k] == -INFINITY ? 1.0f : half_power(m[k] - to);
+            l[k] = l[k] * h * h;
+            total += l[k];
+        }
+        const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+        r *= before * inv;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) r += x[k] * (l[k] * inv);
+        top = to;
     }
     if (lane < LANES) {
         if (ch == 0) stat_lds[0][lane] = top, stat_lds[1][lane] = total;
@@ -436,19 +466,19 @@ template <int DT, int D> __global__ __launch_bounds__(256) void ogc_kv4_attentio
     }
     __syncthreads();
     if (lane > 0) return;
-    // (weighted sums here, not means)
-    const float own = top;
+    float w[LANES];
     for (int k = 0; k < LANES; ++k) top = fmaxf(top, stat_lds[0][k]);
-    const float mine = own == -INFINITY ? 1.0f : half_power(own - top);
-    total = total * mine * mine;
-    r = r * mine * mine;
+    total = 0.0f;
 #pragma unroll
-    for (int k = 1; k < LANES; ++k) {
+    for (int k = 0; k < LANES; ++k) {
         const float m = stat_lds[0][k], h = m == -INFINITY ? 1.0f : half_power(m - top);
-        total += stat_lds[1][k] * h * h;
-        r += *(const v4f*)&o_lds[k][ch] * h * h;
+        w[k] = stat_lds[1][k] * h * h;
+        total += w[k];
     }
-    if (total != 0.0f) r *= 1.0f / total;
+    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+    r = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < LANES; ++k) r += *(const v4f*)&o_lds[k][ch] * (w[k] * inv);
     uint8_t* p = a.o + (s.row0 + i) * a.so[0] + hd * a.so[1] + ch * (DT == OGC_F32 ? 4 : 2);
     if constexpr (DT == OGC_F32) *(v4f*)p = r;
     else *(v2u*)p = (v2u){pack_bf16(r[0], r[1]), pack_bf16(r[2], r[3])};

@@ -1,9 +1,11 @@
-"""The decoder's attention block at the ends of what its inputs may be.  Oracle and
+"""The decoder's attention block at the ends of what its inputs may be: the largest and smallest values, queries and lengths.  Oracle and
 tolerances: test_gpu_decoder.py."""
 import numpy as np
 import pytest
 
-from test_gpu_decoder import torch_
+from oracle import decoder
+from paper_2301_01333_amd import binding
+from test_gpu_decoder import Paged, empty, inside, ints, rows_of, stream, sums, tolerance, torch_, two, untouched
 from test_gpu_decoder_kernels import prompts, streams
 
 pytestmark = pytest.mark.gpu
@@ -30,3 +32,60 @@ def test_prompt_infinite_last_values(dtype, d, many, qs, ks, causal):
         assert (seen[..., 3] == float("inf")).all() and (seen[..., d - 1] == float("-inf")).all()
         assert torch.isfinite(o[at:at + a, :, 4:d - 1]).all() and (not causal or torch.isfinite(o[at:at + a - 1]).all())
         at += a
+
+
+# ---- attention over the cache -----------------------------------------------------------------------------------------------
+def ask(dtype, c, q, fresh, lens, scale, shared):
+    """What the queries q get; shared: whether several workgroups have a sequence."""
+    torch = torch_()
+    n, hq, d = q.shape
+    raw, o = empty(n, hq, d, dtype)
+    cu, ln = sums(fresh), ints(lens)
+    desc = binding.kv4_attention_desc(binding.DTYPES[dtype], hq, n, max(fresh), max(lens), scale, two(q), two(o))
+    need = binding.ogc_kv4_attention_workspace_bytes(c.desc, desc)
+    assert (need > 0) == shared
+    ws = torch.full((max(16, need),), 0xFF, dtype=torch.uint8, device="cuda")
+    binding.ogc_kv4_attention_run(c.desc, desc, q.data_ptr(), cu.data_ptr(), ln.data_ptr(), c.table.data_ptr(), c.device.data_ptr(), o.data_ptr(), ws.data_ptr(), stream())
+    torch.cuda.synchronize()
+    assert untouched(raw)
+    return o
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shared", [True, False])
+@pytest.mark.parametrize("d,late", [(64, False), (96, True), (128, True)])
+def test_step_sums_of_the_largest_values(dtype, shared, d, late):
+    """Thousands of values near the largest that there is have a finite mean, whatever their sum is; channels of the smallest ones beside them keep their
+    digits.  late: the scores grow slowly, so that the weights are above those that their reference has."""
+    torch = torch_()
+    rng = np.random.default_rng(d)
+    n, heads, batch = 4000, 2, 1
+    if not shared:  # enough workgroups without splits
+        heads, batch = 8, 96
+    lens = [n] + [1 + i % 5 for i in range(batch - 1)]
+    print("case: largest values", dtype, shared, d, late, flush=True)
+    c = Paged(rng, lens, heads, d, 64)
+    data = c.oracle.data
+    data[..., :16 * d] = rng.integers(0, 256, data[..., :16 * d].shape)
+    data[..., 16 * d:32 * d] = rng.integers(0, 256, data[..., 16 * d:32 * d].shape) & 0x77 | 0x44   # 2 .. 6, all above zero
+    data[..., 32 * d:33 * d] = 122
+    data[..., 33 * d:33 * d + 32] = 252          # 2^125 ..
+    data[..., 33 * d + 32:34 * d] = 5            # ... and 2^-122
+    if late:  # channel 0 of the keys is the only one, and grows over sixteen pages, a wavefront's share
+        data[..., :16 * d] = 0
+        for e in range(c.rows.shape[1]):
+            for b in range(batch):
+                if c.rows[b, e] >= 0:
+                    data[c.rows[b, e], :, :, 0:16 * d:d // 2] = 2
+                    data[c.rows[b, e], :, :, 32 * d:32 * d + 32] = 126 + e % 16 // 4
+    c.device.copy_(torch.from_numpy(data))
+    q, q64 = rows_of(rng, batch, heads, d, dtype, "plain", 0.5)
+    if late:
+        q.fill_(10.0)
+        q64 = q.double().cpu().numpy()
+    o = ask(dtype, c, q, [1] * batch, lens, 0.125, shared)
+    for b, m in enumerate(lens[:4]):
+        k, v, _ = c.tokens(b, m)
+        want = decoder.attend(q64[b:b + 1], k, v, np.ones((1, m), dtype=bool), 0.125)
+        assert np.isfinite(want[0]).all()
+        inside(o[b:b + 1], want[0], tolerance(dtype, *want, m, d), "sequence %d" % b)
