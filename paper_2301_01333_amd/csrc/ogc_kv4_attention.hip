@@ -136,9 +136,9 @@ template <int DT, int D32, int T, int W> __global__ __launch_bounds__(64 * W, st
     const uint32_t x = blockIdx.x;
     const int head = x % (uint32_t)a.heads, y = x / (uint32_t)a.heads, split = y / (uint32_t)a.columns, c0 = y % (uint32_t)a.columns * 16 * T;
     const StepSequence s = sequence_of(a, b);
-    const int k0 = split * a.chunk;  // (the host holds splits * chunk below 2^31)
+    const int k0 = split * a.chunk;  // (below max_keys)
     if (c0 >= s.n * a.group || (split > 0 && k0 >= s.len)) return;
-    const int k1 = min(s.len, k0 + a.chunk);
+    const int k1 = kv4_split_end(s.len, a.chunk, k0);
 
     // ---- queries: the second operand of the first product, in one or three bf16 pieces
     v8bf q[T][P][D32];
@@ -424,7 +424,7 @@ template <int DT, int D> __global__ __launch_bounds__(256) void ogc_kv4_attentio
     const uint32_t heads = a.heads * a.group;
     const int ch = threadIdx.x % CH * 4, lane = threadIdx.x / CH, hd = blockIdx.x % heads, i = blockIdx.x / heads;
     if (i >= s.n) return;
-    const int n = (s.len + a.chunk - 1) / a.chunk;
+    const int n = kv4_splits_of(s.len, a.chunk);
     const long long at = (long long)(s.row0 + i) * heads + hd, step = (long long)a.rows * heads;
     float top = -INFINITY, total = 0.0f;
     v4f r = {0.0f, 0.0f, 0.0f, 0.0f};  // the mean so far

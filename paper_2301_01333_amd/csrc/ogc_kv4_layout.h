@@ -34,4 +34,9 @@ KV4_FN int64_t kv4_record_at(const int32_t* entries, int width, int page_size, i
     return (((int64_t)page * heads + head) * (page_size / KV4_TOKENS) + position % page_size / KV4_TOKENS) * kv4_record_bytes(d);
 }
 
+// The splits of a sequence of `len` tokens, `chunk` tokens each, and where the one that begins at k0 (0, or below len) ends.  Both numbers may be near
+// 2^31: they are never added up.
+KV4_FN int kv4_splits_of(int len, int chunk) { return len > 0 ? (len - 1) / chunk + 1 : 0; }
+KV4_FN int kv4_split_end(int len, int chunk, int k0) { return len - k0 > chunk ? k0 + chunk : len; }
+
 #endif

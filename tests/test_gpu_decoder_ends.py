@@ -89,3 +89,27 @@ def test_step_sums_of_the_largest_values(dtype, shared, d, late):
         want = decoder.attend(q64[b:b + 1], k, v, np.ones((1, m), dtype=bool), 0.125)
         assert np.isfinite(want[0]).all()
         inside(o[b:b + 1], want[0], tolerance(dtype, *want, m, d), "sequence %d" % b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_step_longest_sequence(dtype):
+    """A sequence of all the tokens that a page table may stand for, with pages for its first and its last ones only."""
+    torch = torch_()
+    rng = np.random.default_rng(4)
+    d, page, held = 32, 512, 0x7fff0000
+    width = held // page
+    print("case: longest sequence", dtype, flush=True)
+    c = Paged(rng, [2 * page], 1, d, page, spare=1)
+    c.oracle.data[..., 32 * d:] = 125
+    c.device.copy_(torch.from_numpy(c.oracle.data))
+    k, v, _ = c.tokens(0, 2 * page)
+    first, last = c.rows[0]
+    c.table = torch.full((1, width), -1, dtype=torch.int32, device="cuda")
+    c.table[0, 0], c.table[0, width - 1] = int(first), int(last)
+    c.desc = binding.kv4_desc(1, d, page, c.pages, 1, width)
+    q, q64 = rows_of(rng, 2, 3, d, dtype, "plain")
+    o = ask(dtype, c, q, [2], [held], 0.125, True)
+    vis = np.ones((2, 2 * page), dtype=bool)
+    vis[0, -1] = False
+    want = decoder.attend(q64, k, v, vis, 0.125)
+    inside(o, want[0], tolerance(dtype, *want, 2 * page, d), "the longest")
