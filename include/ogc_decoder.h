@@ -102,8 +102,8 @@ ogc_status ogc_kv4_read(const ogc_kv4_desc* cache_desc, const ogc_kv4_rows* rows
  *     o[i] = sum_j p[j] v[j] / sum_j p[j],   p[j] = exp(scale * q[i] . k[j] - reference)
  * Query heads h * q_heads / kv_heads .. share the key head h.  Products of bf16 values with fp32 sums (codes times a power of two
  * are bf16 values as they are); OGC_BF16 rounds the weights to bf16 for the second product and adds up the rounded ones, OGC_F32
- * splits queries and weights into three bf16 values without loss.  A query that sees nothing gets zeros.  Values whose scale is 2^-127
- * count as zero here. */
+ * splits queries and weights into three bf16 values, without loss but for channels of a query below 2^-64 of its largest one.  A query that
+ * sees nothing gets zeros.  Values whose scale is 2^-127 count as zero here. */
 typedef struct ogc_kv4_attention_desc {
     int32_t dtype;          /* of q and o */
     int32_t q_heads;        /* a multiple of kv_heads, at most 256 times it */

@@ -140,8 +140,11 @@ template <int DT, int D32, int T, int W> __global__ __launch_bounds__(64 * W, st
     if (c0 >= s.n * a.group || (split > 0 && k0 >= s.len)) return;
     const int k1 = kv4_split_end(s.len, a.chunk, k0);
 
-    // ---- queries: the second operand of the first product, in one or three bf16 pieces
+    // ---- queries: the second operand of the first product, in one or three bf16 pieces.  Three pieces hold an fp32 value from 2^-110 on, and below
+    // bf16's largest: a query whose largest channel is below 2^-46 or from 2^64 on is multiplied by a power of two, which its scores' scale takes out
+    // again, so that only channels 2^-64 times that large can lose digits.
     v8bf q[T][P][D32];
+    float by[T];  // the scores' scale, base-2 logarithms
     int limit[T];  // the last token that this lane's column sees
     float ref[T], sum[T];
     v4f out[T][D32][2];
@@ -151,14 +154,28 @@ template <int DT, int D32, int T, int W> __global__ __launch_bounds__(64 * W, st
         const bool on = i < s.n;
         limit[t] = on ? s.off + i : -1;
         const uint8_t* p = a.q + (long long)(s.row0 + (on ? i : 0)) * a.sq[0] + (long long)(head * a.group + c - i * a.group) * a.sq[1] + g * D32 * 8 * E;
+        by[t] = a.scale_log2;
+        if constexpr (P == 1) {
+            const v4i z = {0, 0, 0, 0};
 #pragma unroll
-        for (int d = 0; d < D32; ++d) {
-            if constexpr (P == 1) {
-                const v4i z = {0, 0, 0, 0};
-                q[t][0][d] = __builtin_bit_cast(v8bf, on ? *(const v4i*)(p + d * 16) : z);
-            } else {
-                const v4f z = {0.0f, 0.0f, 0.0f, 0.0f};
-                const Pieces8 r = split8(on ? *(const v4f*)(p + d * 32) : z, on ? *(const v4f*)(p + d * 32 + 16) : z);
+            for (int d = 0; d < D32; ++d) q[t][0][d] = __builtin_bit_cast(v8bf, on ? *(const v4i*)(p + d * 16) : z);
+        } else {
+            const v4f z = {0.0f, 0.0f, 0.0f, 0.0f};
+            v4f x[2 * D32];
+            float most = 0.0f;
+#pragma unroll
+            for (int d = 0; d < 2 * D32; ++d) {
+                x[d] = on ? *(const v4f*)(p + d * 16) : z;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) most = fmaxf(most, fabsf(x[d][e]));
+            }
+            most = fmaxf(most, __shfl_xor(most, 16));
+            most = fmaxf(most, __shfl_xor(most, 32));
+            const float up = most < 0x1p-46f ? 0x1p64f : most >= 0x1p64f ? 0x1p-64f : 1.0f;
+            by[t] *= most < 0x1p-46f ? 0x1p-64f : most >= 0x1p64f ? 0x1p64f : 1.0f;
+#pragma unroll
+            for (int d = 0; d < D32; ++d) {
+                const Pieces8 r = split8(x[2 * d] * up, x[2 * d + 1] * up);
 #pragma unroll
                 for (int i = 0; i < 3; ++i) q[t][i][d] = __builtin_bit_cast(v8bf, r.p[i]);
             }
@@ -265,7 +282,7 @@ again:
                     cand = fmaxf(cand, e[t][j]);
                 }
             }
-            cand *= a.scale_log2;  // (positive)
+            cand *= by[t];  // (positive)
             // The reference of the exponentials only has to be near the maximum: it moves where a block exceeds it by 2^8.
             if (__builtin_amdgcn_ballot_w64(cand > ref[t] + 8.0f) != 0) {
                 cand = fmaxf(cand, __shfl_xor(cand, 16));
@@ -280,7 +297,7 @@ again:
             }
             const float off = ref[t] == -INFINITY ? 0.0f : factor - ref[t];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) e[t][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(e[t][j], a.scale_log2, off));
+            for (int j = 0; j < 8; ++j) e[t][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(e[t][j], by[t], off));
             if constexpr (P == 1) {  // rounded once; the sum takes what the second product multiplies
 #pragma unroll
                 for (int j = 0; j < 8; j += 2) {

@@ -91,6 +91,35 @@ def test_step_sums_of_the_largest_values(dtype, shared, d, late):
         inside(o[b:b + 1], want[0], tolerance(dtype, *want, m, d), "sequence %d" % b)
 
 
+@pytest.mark.parametrize("shared", [True, False])
+@pytest.mark.parametrize("size,byte,scale", [(2.0 ** -120, 246, 0.125), (2.0 ** -146, 252, 2.0 ** 18), (2.0 ** 64, 63, 0.125), (3.402e38, 2, 2.0 ** -5)])
+def test_step_small_and_large_fp32_queries(shared, size, byte, scale):
+    """Queries at both ends of fp32 whose scores are ordinary, as the keys are at the other end: all their digits count."""
+    torch = torch_()
+    rng = np.random.default_rng(byte)
+    d, hk, hq = 96, 2, 4
+    lens = [1500, 40, 7] if shared else [300, 40, 7]
+    print("case: queries of", size, shared, flush=True)
+    c = Paged(rng, lens, hk, d, 64)
+    c.oracle.data[..., 32 * d:33 * d] = byte
+    c.oracle.data[..., 33 * d:34 * d] = 127
+    c.device.copy_(torch.from_numpy(c.oracle.data))
+    x = rng.uniform(-1, 1, (6, hq, d)) * size
+    x[1] *= 2.0 ** -3 if size < 1 else 2.0 ** -9
+    x[2, :, 7] = size * (1 - 2.0 ** -24)
+    q = torch.from_numpy(x).float().cuda()
+    assert torch.isfinite(q).all()
+    fresh, q64 = [3, 1, 2], q.double().cpu().numpy()
+    o = ask("f32", c, q, fresh, lens, scale, shared)
+    i = 0
+    for b, m in enumerate(fresh):
+        k, v, _ = c.tokens(b, lens[b])
+        vis = np.arange(lens[b])[None, :] <= np.arange(m)[:, None] + (lens[b] - m)
+        want = decoder.attend(q64[i:i + m], k, v, vis, scale)
+        inside(o[i:i + m], want[0], tolerance("f32", *want, lens[b], d), "sequence %d" % b)
+        i += m
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_step_longest_sequence(dtype):
     """A sequence of all the tokens that a page table may stand for, with pages for its first and its last ones only."""
