@@ -114,7 +114,8 @@ typedef struct ogc_kv4_attention_desc {
 } ogc_kv4_attention_desc;
 
 ogc_status ogc_kv4_attention_validate(const ogc_kv4_desc* cache_desc, const ogc_kv4_attention_desc* desc);
-/* Bytes that a call needs at `workspace` (0: none), for sequences shared by several workgroups. */
+/* Bytes that a call needs at `workspace` (0: none), for sequences shared by several workgroups.  They are enough for the same call with
+ * fewer max_keys, too: a workspace for the longest that a cache will hold can be kept as it fills. */
 ogc_status ogc_kv4_attention_workspace_bytes(const ogc_kv4_desc* cache_desc, const ogc_kv4_attention_desc* desc, size_t* bytes);
 /* q, o: packed rows; o is written for all of them and must not overlap the inputs.  lens: device int32 [batch].  workspace: 16-byte
  * aligned, contents do not matter. */

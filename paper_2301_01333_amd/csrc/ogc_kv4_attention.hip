@@ -531,7 +531,9 @@ StepShape shape_of(const ogc_kv4_desc* c, const ogc_kv4_attention_desc* d) {
     if (s.waves == 8) chunk = keys;
     s.splits = keys > 0 ? (int)((keys + chunk - 1) / chunk) : 1;
     s.chunk = (int)(s.splits == 1 ? 0x7fffffff / 512 * 512 : chunk);
-    s.bytes = s.splits > 1 ? (size_t)s.splits * d->rows * d->q_heads * (c->head_dim + 2) * 4 : 0;
+    // (enough for any fewer tokens, which may be cut into more splits than these; where they have no splits fewer have none either)
+    const int64_t most = want < (keys + least - 1) / least ? want : (keys + least - 1) / least;
+    s.bytes = s.splits > 1 ? (size_t)most * d->rows * d->q_heads * (c->head_dim + 2) * 4 : 0;
     return s;
 }
 

@@ -37,7 +37,11 @@ class DecoderAttention:
         half = torch.arange(0, self.rot_dim, 2, dtype=torch.float64, device="cuda")
         self.frequencies = theta ** (-half / max(self.rot_dim, 1))
         self.one_each = torch.arange(batch + 1, dtype=torch.int32, device="cuda")
-        self.workspace = torch.empty(256, dtype=torch.uint8, device="cuda")
+        # for all steps, of any length: it never moves while a step or a captured graph may be using it
+        each = (q_heads * head_dim, head_dim)
+        longest = binding.kv4_attention_desc(self.dtype, q_heads, batch, 1, max_tokens, head_dim ** -0.5, each, each)
+        need = binding.ogc_kv4_attention_workspace_bytes(self.cache_desc, longest)
+        self.workspace = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
 
     def _turned(self, qkv, positions):
         torch, n, hq, hk = self.torch, qkv.shape[0], self.q_heads, self.kv_heads
@@ -91,9 +95,6 @@ class DecoderAttention:
         self.held += 1
         o = torch.empty_like(q)
         desc = binding.kv4_attention_desc(self.dtype, self.q_heads, self.batch, 1, self.held, self.head_dim ** -0.5, q.stride()[:2], o.stride()[:2])
-        need = binding.ogc_kv4_attention_workspace_bytes(self.cache_desc, desc)
-        if need > self.workspace.numel():
-            self.workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
         binding.ogc_kv4_attention_run(self.cache_desc, desc, q.data_ptr(), self.one_each.data_ptr(), self.lens.data_ptr(), self.table.data_ptr(),
                                       self.cache.data_ptr(), o.data_ptr(), self.workspace.data_ptr(), self._stream())
         return o
