@@ -112,6 +112,10 @@ def lib():
         if not os.path.exists(LIB_PATH):
             raise FileNotFoundError(
                 "%s not found: build it with `python -m paper_2301_01333_amd.build` (there is no fallback path)" % LIB_PATH)
+        try:  # PyTorch brings a HIP runtime of its own: loaded after this library, it would be a second one, whose streams and memory launches do not know
+            import torch  # noqa: F401
+        except ImportError:
+            pass
         l = ctypes.CDLL(LIB_PATH)
         vp, i32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
         l.ogc_mlp_plan.argtypes = [ctypes.POINTER(ogc_mlp_desc), ctypes.POINTER(vp)]
