@@ -12,6 +12,27 @@ from typing import Optional, Sequence
 from . import binding
 
 
+def check_rows(qkv, dtype, heads: int, head_dim: int, device) -> None:
+    """ValueError unless qkv is rows as a layer's calls take them: the kernels get an address and strides, and believe them."""
+    if qkv.dim() != 3 or tuple(qkv.shape[1:]) != (heads, head_dim):
+        raise ValueError("rows of shape %s, not [tokens, %d, %d]" % (list(qkv.shape), heads, head_dim))
+    if qkv.dtype != dtype:
+        raise ValueError("rows of type %s, not %s" % (qkv.dtype, dtype))
+    if qkv.stride(2) != 1:
+        raise ValueError("the channels of a head are %d elements apart, not next to each other" % qkv.stride(2))
+    if qkv.device != device:
+        raise ValueError("rows on %s, not on %s" % (qkv.device, device))
+
+
+def check_weights(q_weight, k_weight, dtype, head_dim: int) -> None:
+    """ValueError unless there are weights of the type for queries and keys, or for neither."""
+    if (q_weight is None) != (k_weight is None):
+        raise ValueError("weights of the norms of queries and of keys, or neither")
+    for w in (q_weight, k_weight):
+        if w is not None and (w.dtype != dtype or tuple(w.shape) != (head_dim,) or not w.is_contiguous()):
+            raise ValueError("a norm's weight of type %s and shape %s, not %s [%d], contiguous" % (w.dtype, list(w.shape), dtype, head_dim))
+
+
 class DecoderAttention:
     """The attention of one layer for `batch` sequences of up to `max_tokens` tokens, whose keys and values are held in 4 bits.
 
@@ -23,11 +44,16 @@ class DecoderAttention:
                  eps: float = 1e-6):
         import torch
 
+        if dtype not in ("f32", "bf16"):
+            raise ValueError("type %s, not f32 or bf16" % (dtype,))
+        check_weights(q_weight, k_weight, torch.float32, head_dim)
         self.torch, self.dtype = torch, binding.DTYPES[dtype]
         self.torch_dtype = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
         self.q_heads, self.kv_heads, self.head_dim, self.batch, self.max_tokens = q_heads, kv_heads, head_dim, batch, max_tokens
         self.rot_dim, self.layout, self.eps = head_dim if rot_dim is None else rot_dim, layout, eps
         self.q_weight, self.k_weight = q_weight, k_weight
+        if q_weight is not None and not (q_weight.is_cuda and k_weight.is_cuda):
+            raise ValueError("the norms' weights are on %s and %s, not on the GPU" % (q_weight.device, k_weight.device))
         width = -(-max_tokens // page_size)
         self.cache_desc = binding.kv4_desc(kv_heads, head_dim, page_size, batch * width, batch, width)
         self.cache = torch.zeros(binding.ogc_kv4_cache_bytes(self.cache_desc), dtype=torch.uint8, device="cuda")
@@ -66,14 +92,15 @@ class DecoderAttention:
     def prefill(self, qkv, lengths: Sequence[int]):
         """The prompts of empty sequences, packed; lengths: of all of them (zero: none)."""
         torch, hq, d = self.torch, self.q_heads, self.head_dim
-        if len(lengths) != self.batch or sum(lengths) != qkv.shape[0] or max(lengths) > self.max_tokens:
+        check_rows(qkv, self.torch_dtype, hq + 2 * self.kv_heads, d, self.cache.device)
+        if len(lengths) != self.batch or sum(lengths) != qkv.shape[0] or min(lengths) < 0 or max(lengths) > self.max_tokens:
             raise ValueError("lengths %s do not fit %d sequences of up to %d tokens and %d rows" % (
                 list(lengths), self.batch, self.max_tokens, qkv.shape[0]))
         ends = torch.tensor([0] + list(lengths), dtype=torch.int32).cumsum(0, dtype=torch.int32)
         cu = ends.cuda()
         positions = torch.cat([torch.arange(n, dtype=torch.int32) for n in lengths]).cuda()
+        q, k, v = self._turned(qkv, positions)  # (a call that is refused leaves the layer as it is)
         self.lens.zero_()
-        q, k, v = self._turned(qkv, positions)
         longest = max(lengths)
         self._append(k, v, cu, longest)
         o = torch.empty_like(q)
@@ -87,6 +114,7 @@ class DecoderAttention:
     def step(self, qkv):
         """One more token of every sequence, row b sequence b's."""
         torch = self.torch
+        check_rows(qkv, self.torch_dtype, self.q_heads + 2 * self.kv_heads, self.head_dim, self.cache.device)
         if qkv.shape[0] != self.batch or self.held >= self.max_tokens:
             raise ValueError("%d rows for %d sequences, the longest of %d tokens of %d" % (qkv.shape[0], self.batch, self.held, self.max_tokens))
         q, k, v = self._turned(qkv, self.lens)
