@@ -11,7 +11,7 @@
  * so that the slices of one projection's output work as they are.  Strides are multiples of 16 bytes, bases 16-byte aligned.
  * The rows of several sequences are packed: sequence b has the rows cu[b] .. cu[b + 1] - 1 (cu: device int32 [batch + 1], ascending
  * from 0).  The number of rows and the longest sequence are given by the host, because launches are sized by them: a sequence's rows
- * beyond the longest that was announced are left out, and indices beyond the number of rows are cut to it.
+ * beyond the longest that was announced are left out (a prompt's keys are not), and indices beyond the number of rows are cut to it.
  *
  * Types: OGC_F32 and OGC_BF16.  Sums, norms, softmax statistics and angles are held in 32 bits or more; bf16 results are rounded once,
  * to nearest even.  head_dim is 32, 64, 96 or 128, of all operators.
@@ -134,7 +134,7 @@ typedef struct ogc_prompt_desc {
     int32_t q_heads, kv_heads;  /* > 0; q_heads a multiple of kv_heads, at most 256 times it */
     int32_t head_dim;
     int32_t q_rows, k_rows;     /* of all sequences, >= 0 */
-    int32_t max_q, max_k;       /* of the longest, >= 0 */
+    int32_t max_q, max_k;       /* of the longest, >= 0; max_k orders the work and no more: keys beyond it are seen, and too large a one costs nothing */
     float scale;                /* 2^-60 .. 2^60 */
     int32_t causal;             /* 1, or 0: every query sees every key of its sequence */
     int64_t q_stride[2], k_stride[2], v_stride[2], o_stride[2];

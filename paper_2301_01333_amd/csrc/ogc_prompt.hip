@@ -9,6 +9,7 @@
 // The tiles that reach furthest start first.
 #include "ogc_attention.h"
 #include "ogc_decoder.h"
+#include "ogc_prompt_tiles.h"
 
 #include <stdio.h>
 #include <type_traits>
@@ -24,7 +25,7 @@ struct PromptArgs {
     int q_rows, k_rows, max_q;
     int batch, heads, group;  // key heads, query heads of each
     int causal;
-    int level_keys;           // keys of one of the 64 levels by which tiles are sorted
+    int level_keys;           // keys of one of the levels by which tiles are sorted
     float scale_log2;
 };
 
@@ -61,19 +62,10 @@ MHA_DEV int sum_to_lane(int x) {
     x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
     return x;
 }
-// Tiles of a sequence that reach key x or further (level 0: all of them).
 template <int ROWS> MHA_DEV int tiles_from(const PromptArgs& a, const PromptSequence& s, int level) {
-    const int rows = s.n * a.group, tiles = (rows + ROWS - 1) / ROWS;
-    if (level <= 0) return tiles;
-    if (level > 63) return 0;
-    const int x = level * a.level_keys;
-    if (!a.causal) return s.m - 1 >= x ? tiles : 0;
-    const int i = x - s.off;  // the first query that does
-    if (i >= s.n) return 0;
-    if (i <= 0) return tiles;
-    return tiles - i * a.group / ROWS;
+    return prompt_tiles_from(s.n, s.m, s.off, a.group, a.causal, level, a.level_keys, ROWS);
 }
-// The tile of this workgroup.  The tiles of all sequences are handed out from the one that reaches furthest on, sorted in 64 levels, so that no
+// The tile of this workgroup.  The tiles of all sequences are handed out from the one that reaches furthest on, sorted in PROMPT_LEVELS levels, so that no
 // workgroup but the last few is without work: workgroups are dealt to the parts of the chip in turn, whether they have work or not, and
 // a grid with a place for each sequence's every possible tile left whole parts idle (8 prompts of 370 .. 4096 tokens, 32 heads over 8 of 128 channels: 595 us, so 467).
 // A lane counts the tiles of a sequence; the level and then the sequence are found from the sums.  (Heads go round the 8 XCDs: with a multiple
@@ -96,7 +88,7 @@ template <int ROWS> MHA_DEV bool tile_of(const PromptArgs& a, PromptTile& t) {
         };
         if (j >= all_from(0)) return false;
         int level = 0, above = 0;  // the highest level from which on there are more than j tiles, and those above it
-        for (int step = 32; step > 0; step /= 2) {
+        for (int step = PROMPT_LEVELS / 2; step > 0; step /= 2) {
             const int c = all_from(level + step);
             if (c > j) level += step;
             else above = c;
@@ -282,7 +274,7 @@ ogc_status ogc_prompt_run(const ogc_prompt_desc* d, const void* q, const void* k
     a.group = d->q_heads / d->kv_heads;
     a.causal = d->causal;
     a.scale_log2 = d->scale * LOG2E;
-    a.level_keys = d->max_k / 64 + 1;
+    a.level_keys = prompt_level_keys(d->max_k, d->k_rows);
     const bool few = few_case(d);
     const dim3 grid((unsigned)(tiles_of(d, few ? PROMPT_FEW : PROMPT_ROWS) * a.heads));
     if (few) {

@@ -39,3 +39,48 @@ int main() {
     return 0;
 }
 """)
+
+
+def test_tiles_by_how_far_they_reach(tmp_path):
+    """Against a count where there are few; and where there are more queries than keys by far, fewer tiles from level to level, and none twice."""
+    runs(tmp_path, r"""
+#include "ogc_prompt_tiles.h"
+#include <stdio.h>
+#include <initializer_list>
+int main() {
+    for (int n : {0, 1, 5, 33, 200})
+        for (int m : {0, 1, 4, 64, 65, 300, 1000})
+            for (int group : {1, 3, 8})
+                for (int rows : {32, 128})
+                    for (int causal : {0, 1})
+                        for (int max_k : {0, 64, 1000, 0x7fff0000}) {
+                            const int keys = prompt_level_keys(max_k, 1000), off = m - n;
+                            for (int level = 0; level <= PROMPT_LEVELS; ++level) {
+                                int count = 0;
+                                for (int t = 0; t * rows < n * group; ++t) {
+                                    const int last = t * rows + rows < n * group ? t * rows + rows - 1 : n * group - 1;
+                                    const int reach = causal ? last / group + off : m - 1;
+                                    count += level == 0 || (level < PROMPT_LEVELS && reach >= level * keys);
+                                }
+                                const int got = prompt_tiles_from(n, m, off, group, causal, level, keys, rows);
+                                if (got != count) return printf("%d queries, %d keys, group %d: %d tiles from level %d, not %d\n", n, m, group, got, level, count), 1;
+                            }
+                        }
+    for (int n : {1 << 20, 1 << 30, 0x7fff0000 - 100})
+        for (int m : {0, 100, 1 << 20})
+            for (int whole : {n, 0x7fff0000})  // of queries: those beyond the announced longest are left out
+                for (int keys : {prompt_level_keys(0x7fff0000, m), prompt_level_keys(0x7fff0000, 0x7fff0000)}) {
+                    int last = prompt_tiles_from(n, m, m - whole, 1, 1, 0, keys, 128);
+                    if (last != (n + 127) / 128) return puts("all"), 1;
+                    for (int level = 1; level <= PROMPT_LEVELS; ++level) {
+                        const int got = prompt_tiles_from(n, m, m - whole, 1, 1, level, keys, 128);
+                        const int64_t first = (int64_t)level * keys - (m - whole), want = level == PROMPT_LEVELS || first >= n ? 0 : first <= 0 ? last : (n + 127) / 128 - first / 128;
+                        if (got > last || got != want) return printf("%d queries, %d keys: %d tiles from level %d after %d\n", n, m, got, level, last), 1;
+                        last = got;
+                    }
+                }
+    if (prompt_level_keys(0x7fff0000, 640) != 11 || prompt_level_keys(640, 0x7fff0000) != 11) return puts("levels"), 1;
+    puts("ok");
+    return 0;
+}
+""")

@@ -142,3 +142,26 @@ def test_step_longest_sequence(dtype):
     vis[0, -1] = False
     want = decoder.attend(q64, k, v, vis, 0.125)
     inside(o, want[0], tolerance(dtype, *want, 2 * page, d), "the longest")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("announced", [0, 7, 0x7fff0000])
+def test_prompt_keys_are_seen_whatever_was_announced(dtype, announced):
+    """The announced longest of the keys orders the work and no more."""
+    torch = torch_()
+    rng = np.random.default_rng(12)
+    qs, ks, d = [40, 300, 1], [90, 300, 700], 64
+    print("case: announced keys", dtype, announced, flush=True)
+    (q, q64), (k, k64), (v, v64) = (rows_of(rng, rows, 2, d, dtype, "plain") for rows in (sum(qs), sum(ks), sum(ks)))
+    raw, o = empty(sum(qs), 2, d, dtype)
+    cq, ck = sums(qs), sums(ks)
+    desc = binding.prompt_desc(binding.DTYPES[dtype], 3, 2, 2, d, sum(qs), sum(ks), max(qs), announced, 0.125, 1, two(q), two(k), two(v), two(o))
+    binding.ogc_prompt_run(desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), cq.data_ptr(), ck.data_ptr(), o.data_ptr(), stream())
+    torch.cuda.synchronize()
+    i = j = 0
+    for a, b in zip(qs, ks):
+        vis = np.arange(b)[None, :] <= np.arange(a)[:, None] + (b - a)
+        want = decoder.attend(q64[i:i + a], k64[j:j + b], v64[j:j + b], vis, 0.125)
+        inside(o[i:i + a], want[0], tolerance(dtype, *want, b, d), "sequence of %d and %d" % (a, b))
+        i, j = i + a, j + b
+    assert untouched(raw)
