@@ -216,6 +216,8 @@ template <bool WRITE, int DT, int D> void launch(const StoreArgs& a, dim3 grid, 
     if constexpr (WRITE) hipLaunchKernelGGL((ogc_kv4_write_kernel<DT, D>), grid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL((ogc_kv4_read_kernel<DT, D>), grid, dim3(256), 0, st, a);
 }
+// Octets of tokens of the longest sequence: one more than its tokens make, where it starts at no multiple of eight.
+int64_t octets_of(const ogc_kv4_rows* r) { return ((int64_t)(r->max_rows < r->rows ? r->max_rows : r->rows) + 7) / 8 + 1; }
 template <bool WRITE> ogc_status move(const ogc_kv4_desc* c, const ogc_kv4_rows* r, const void* k, const void* v, const void* cache,
                                       const int32_t* cu, const int32_t* start, const int32_t* table, void* stream) {
     const ogc_status st = ogc_kv4_validate(c, r);
@@ -242,10 +244,8 @@ template <bool WRITE> ogc_status move(const ogc_kv4_desc* c, const ogc_kv4_rows*
     a.page_size = c->page_size;
     a.pages = c->pages;
     a.width = c->table_width;
-    a.octets = (int)(((int64_t)a.max_rows + 7) / 8 + 1);  // (one more where the start is no multiple of eight)
-    const int64_t waves = (int64_t)a.octets * a.heads;
-    if (waves > 0x7ffffff0) return OGC_ERR_SHAPE;
-    const dim3 grid((unsigned)((waves + 3) / 4), (unsigned)c->batch);
+    a.octets = (int)octets_of(r);
+    const dim3 grid((unsigned)(((int64_t)a.octets * a.heads + 3) / 4), (unsigned)c->batch);
     const hipStream_t s = (hipStream_t)stream;
     const bool f32 = r->dtype == OGC_F32;
     switch (c->head_dim) {
@@ -276,6 +276,7 @@ ogc_status ogc_kv4_validate(const ogc_kv4_desc* c, const ogc_kv4_rows* r) {
     const ogc_status st = ogc_kv4_check(c);
     if (st != OGC_OK) return st;
     if (r->rows < 0 || r->max_rows < 0) return OGC_ERR_SHAPE;
+    if (octets_of(r) * c->kv_heads > 4 * 0xffffff) return OGC_ERR_SHAPE;  // four a workgroup, and a grid of fewer than 2^32 threads
     if (r->dtype != OGC_F32 && r->dtype != OGC_BF16) return OGC_ERR_UNSUPPORTED;
     const int e = r->dtype == OGC_F32 ? 4 : 2;
     if (!strides_ok(r->k_stride, e) || !strides_ok(r->v_stride, e)) return OGC_ERR_ALIGNMENT;

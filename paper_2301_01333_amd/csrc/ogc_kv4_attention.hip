@@ -577,6 +577,8 @@ ogc_status ogc_kv4_attention_validate(const ogc_kv4_desc* c, const ogc_kv4_atten
     const int max_rows = d->max_rows < d->rows ? d->max_rows : d->rows;
     if ((int64_t)max_rows * d->q_heads > 0x7fffff00) return OGC_ERR_SHAPE;
     if (d->dtype != OGC_F32 && d->dtype != OGC_BF16) return OGC_ERR_UNSUPPORTED;
+    const StepShape s = shape_of(c, d);
+    if ((int64_t)s.splits * s.columns * c->kv_heads * s.waves * 64 > 0xffffffff) return OGC_ERR_SHAPE;  // threads of a grid (a join's are far fewer)
     const int e = d->dtype == OGC_F32 ? 4 : 2;
     if (!strides_ok(d->q_stride, e) || !strides_ok(d->o_stride, e)) return OGC_ERR_ALIGNMENT;
     return OGC_OK;
@@ -628,7 +630,6 @@ ogc_status ogc_kv4_attention_run(const ogc_kv4_desc* c, const ogc_kv4_attention_
     a.splits = s.splits;
     a.columns = s.columns;
     a.scale_log2 = d->scale * LOG2E;
-    if ((int64_t)s.splits * s.columns * a.heads > 0x7fffffff) return OGC_ERR_SHAPE;
     if (d->dtype == OGC_F32) launch_dim<OGC_F32>(c->head_dim / 32, a, s.waves, s.tiles, c->batch, (hipStream_t)stream);
     else launch_dim<OGC_BF16>(c->head_dim / 32, a, s.waves, s.tiles, c->batch, (hipStream_t)stream);
     return hipGetLastError() == hipSuccess ? OGC_OK : OGC_ERR_DEVICE;

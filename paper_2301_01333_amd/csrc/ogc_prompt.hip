@@ -232,10 +232,10 @@ ogc_status ogc_prompt_validate(const ogc_prompt_desc* d) {
     if (d->batch <= 0 || d->q_heads <= 0 || d->kv_heads <= 0 || d->head_dim <= 0) return OGC_ERR_SHAPE;
     if (d->q_rows < 0 || d->k_rows < 0 || d->max_q < 0 || d->max_k < 0) return OGC_ERR_SHAPE;
     if (d->q_heads % d->kv_heads != 0 || d->q_heads / d->kv_heads > 256) return OGC_ERR_SHAPE;
-    // rows of a sequence, keys and their limits stay below 2^31, and so does the grid
+    // rows of a sequence, keys and their limits stay below 2^31, the grid's threads below 2^32
     const int64_t most = d->max_q < d->q_rows ? d->max_q : d->q_rows, group = d->q_heads / d->kv_heads;
     if (most * group > 0x7fff0000 || d->k_rows > 0x7fff0000 - most) return OGC_ERR_SHAPE;
-    if ((int64_t)d->batch * d->kv_heads > 0x7fffffff || tiles_of(d) * d->kv_heads > 0x7fffffff || d->max_k > 0x7fff0000) return OGC_ERR_SHAPE;
+    if (tiles_of(d) * d->kv_heads > 0xffffff || d->max_k > 0x7fff0000) return OGC_ERR_SHAPE;
     if (d->dtype != OGC_F32 && d->dtype != OGC_BF16) return OGC_ERR_UNSUPPORTED;
     if (d->head_dim % 32 != 0 || d->head_dim > 128) return OGC_ERR_UNSUPPORTED;
     const int e = d->dtype == OGC_F32 ? 4 : 2;

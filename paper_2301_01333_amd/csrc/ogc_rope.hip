@@ -196,6 +196,7 @@ ogc_status ogc_rope_validate(const ogc_rope_desc* d) {
     if (!isfinite(d->magnitude)) return OGC_ERR_INVALID_ARG;
     if (d->tokens < 0 || d->q_heads <= 0 || d->kv_heads <= 0 || d->head_dim <= 0 || d->rot_dim < 0 || d->rot_dim > d->head_dim) return OGC_ERR_SHAPE;
     if (d->q_heads > 65536 || d->kv_heads > 65536) return OGC_ERR_SHAPE;
+    if (d->tokens > 4 * 0xffffff) return OGC_ERR_SHAPE;  // four a workgroup (but where they are few), and a grid of fewer than 2^32 threads
     if (d->dtype != OGC_F32 && d->dtype != OGC_BF16) return OGC_ERR_UNSUPPORTED;
     if (d->head_dim % 32 != 0 || d->head_dim > 128 || d->rot_dim % 8 != 0) return OGC_ERR_UNSUPPORTED;
     const int e = d->dtype == OGC_F32 ? 4 : 2;
@@ -250,8 +251,7 @@ ogc_status ogc_rope_run(const ogc_rope_desc* d, const void* q, const void* k, co
     while (a.parts < rounds && (int64_t)d->tokens * a.parts < 4096) ++a.parts;
     a.passes = (rounds + a.parts - 1) / a.parts;
     a.parts = (rounds + a.passes - 1) / a.passes;
-    const int64_t waves = (int64_t)d->tokens * a.parts, grid = (waves + 3) / 4;
-    if (waves > 0x7fffffff) return OGC_ERR_SHAPE;  // (never: more than one a token only where they are few)
+    const int64_t grid = ((int64_t)d->tokens * a.parts + 3) / 4;  // (below 2^24: more than one wavefront a token only where they are few)
     const hipStream_t s = (hipStream_t)stream;
     if (d->dtype == OGC_F32) launch<OGC_F32, 4>(d->head_dim, a, (unsigned)grid, s);
     else if (wide) launch<OGC_BF16, 8>(d->head_dim, a, (unsigned)grid, s);
