@@ -200,13 +200,18 @@ def check_decoder_loops(verbose: bool = True) -> None:
     """The attention kernels over the 4-bit cache and over few prompt tiles count their direct loads: one wait for all but the newest, and one for all
     at the end.  A load of the compiler's own in the loop (a page by the vector unit, the queries waited for in every round, a spilled
     register) would wait for the counted ones: this compiles the kernels to assembly and fails if their loop over the keys waits
-    for vector memory otherwise or touches scratch memory."""
+    for vector memory otherwise or touches scratch memory.  The streaming body counts its loads too, in steps that the compiler lays out as
+    it likes, and the split body's loads run a block ahead: no kernel of the prompts may use scratch memory anywhere."""
     import re
 
     checked = 0
+    text = {source: _device_assembly(source) for source in ("ogc_kv4_attention.hip", "ogc_prompt.hip")}
+    prompts = re.findall(r"\.name:\s+(\w*ogc_prompt_\w*kernel\w+)\s*\n\s+\.private_segment_fixed_size:\s+(\d+)", text["ogc_prompt.hip"])
+    if len(prompts) != 20 or any(int(scratch) for _, scratch in prompts):
+        raise RuntimeError("prompt attention kernels (name, bytes of scratch memory per lane): %s" % prompts)
     for source, name, many in (("ogc_kv4_attention.hip", r"\w*ogc_kv4_attention_kernelI\w*", 24), ("ogc_prompt.hip", r"\w*ogc_prompt_few_kernelI\w*", 4)):
-        text, found = _device_assembly(source), 0
-        for m in re.finditer(r"^(%s):[^\n]*\n(.*?)\n\.Lfunc_end" % name, text, re.S | re.M):
+        found = 0
+        for m in re.finditer(r"^(%s):[^\n]*\n(.*?)\n\.Lfunc_end" % name, text[source], re.S | re.M):
             lines = [l.split(";")[0] for l in m.group(2).splitlines()]
             bodies = [lines[a:b] for a, b in _loops(lines) if any("v_mfma" in l for l in lines[a:b])]
             body = min(bodies, key=len) if bodies else []
@@ -218,7 +223,8 @@ def check_decoder_loops(verbose: bool = True) -> None:
             raise RuntimeError("%s: %d kernels found in the assembly, not %d" % (source, found, many))
         checked += found
     if verbose:
-        print("decoder kernels checked: %d (no waits but the counted ones in the loops over the keys)" % checked, flush=True)
+        print("decoder kernels checked: %d (no waits but the counted ones in the loops over the keys), %d (no scratch memory)" % (
+            checked, len(prompts)), flush=True)
 
 
 if __name__ == "__main__":
