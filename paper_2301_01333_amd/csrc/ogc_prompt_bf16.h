@@ -237,9 +237,10 @@ template <int D32> MHA_DEV void prompt_stream_body(const PromptArgs& a, const Pr
     };
     first_scores(0, s0);
     first_scores(1, s1);
-    // The first reference: the maximum of the first two units, or 0 where the row sees none of their keys (nor any other, then)
+    // The first reference: the maximum of the first two units.  Where there is none the row sees no key at all (0 will do), or its scores there are all
+    // minus infinity: a reference so low that the first finite score counts as far from it.
     const float m = top(s0, s1);
-    ref = m == -INFINITY ? 0.0f : m * c;
+    ref = m == -INFINITY ? (limit < 0 ? 0.0f : -0x1p127f) : m * c;
     step(no, no, 0, s0, s1, w1, w0);
     int u = 1;
     for (; u + 2 < n; u += 2) {

@@ -5,8 +5,8 @@ import pytest
 
 from oracle import decoder
 from paper_2301_01333_amd import binding
-from test_gpu_decoder import Paged, empty, inside, ints, rows_of, stream, sums, tolerance, torch_, two, untouched
-from test_gpu_decoder_kernels import prompts, streams
+from test_gpu_decoder import Paged, dt, empty, inside, ints, rows_of, stream, sums, tolerance, torch_, two, untouched
+from test_gpu_decoder_kernels import WIDE, prompts, streams
 
 pytestmark = pytest.mark.gpu
 
@@ -165,3 +165,31 @@ def test_prompt_keys_are_seen_whatever_was_announced(dtype, announced):
         inside(o[i:i + a], want[0], tolerance(dtype, *want, b, d), "sequence of %d and %d" % (a, b))
         i, j = i + a, j + b
     assert untouched(raw)
+
+
+@pytest.mark.parametrize("body,dtype", [("stream", "bf16"), ("few", "bf16"), ("split", "f32"), ("staged", "bf16"), ("staged", "f32")])
+@pytest.mark.parametrize("d", [32, 64, 96, 128])
+@pytest.mark.parametrize("what", ["lowest", "-inf"])
+def test_prompt_first_scores_beyond_the_range(body, dtype, d, what):
+    """The first seventy keys' scores are minus infinity for every row that sees them (padding of the lowest value, say), all others' far below zero: the rows that
+    see others have the weighted mean of those."""
+    torch = torch_()
+    bad = float("-inf") if what == "-inf" else float(torch.finfo(dt(dtype)).min)
+    qs, ks, far = [100, 40], [170, 40], -300.0
+
+    def spoil(q, k, v):
+        q[:] = q.abs().clamp(0.5, 2.0)
+        k[:] = (k.double() * 0.01 + far / (d ** 0.5 * 1.1)).to(k.dtype)
+        k[:70] = bad
+
+    # (the common check says nothing here: a score that is off by a part of the largest one may be any)
+    seen = {}
+    kernel = {"stream": streams(d), "staged": "ogc_prompt_kernel<%d, %d>" % (binding.DTYPES[dtype], d // 32)}.get(body, "ogc_prompt_%s_kernel<%d>" % (body, d // 32))
+    kw = dict(wide=(WIDE[dtype], 0), copies=1) if body == "staged" else {}
+    o = prompts(kernel, dtype, qs, ks, 2, 1, d, d, spoil=lambda q, k, v: (spoil(q, k, v), seen.update(q=q.clone(), k=k.clone(), v=v.clone())), **kw)
+    q, k, v = (seen[x].double().cpu().numpy() for x in "qkv")
+    scale = float(np.float32(d ** -0.5))
+    vis = np.arange(100)[None, :] <= np.arange(100)[:, None]
+    want = decoder.attend(q[:100], k[70:170], v[70:170], vis, scale)
+    assert np.abs(want[2]).min() > 100
+    inside(o[:100], want[0], tolerance(dtype, *want, 170, d), "the rows' own keys")
