@@ -511,8 +511,10 @@ struct StepShape {
 };
 // How a call is cut.  Columns: 16 or (bf16) 32 a workgroup.  Tokens: into as many splits as give the chip 768 workgroups, the three a compute unit
 // that it holds at a time for 128 channels, of a record for each of four wavefronts at least.  (With 768 / 2048, us, batch x tokens, 32 heads over 8 of
-// 128 channels: 64 x 8192 109 / 114, 32 x up to 4001 30 / 28, 1 x 4000 14 / 12; one of 30000 with 8 x 96 18 / 24.)  Up to 1024 tokens one
-// workgroup of eight wavefronts has them all: no second launch (1 x 1000: 10.2, shared 13.5; at 4000 32, shared 13).
+// 128 channels: 64 x 8192 118 / 120, 32 x up to 4001 29.9 / 28.6, 1 x 4000 13.8 / 13.2; one of 30000 with 8 x 96 17.3 / 22.9.)  Up to 1024 tokens one
+// workgroup of eight wavefronts has them all: no second launch (alone / shared, us, the same heads: 1 x 500 10.1 / 14.2, 1 x 1000 10.5 / 12.7,
+// 1 x 1500 13.3 / 13.3, 1 x 2000 15.3 / 13.4, 4 x up to 2000 15.8 / 13.0; 4 heads of 32: 1 x 1000 9.4 / 12.6, 1 x 2000 10.5 / 12.7; fp32, 8
+// heads of 96: 1 x 500 10.3 / 12.9, 1 x 1000 13.2 / 13.4, 1 x 1500 16.6 / 13.0).
 StepShape shape_of(const ogc_kv4_desc* c, const ogc_kv4_attention_desc* d) {
     StepShape s;
     const int group = d->q_heads / c->kv_heads;

@@ -163,8 +163,9 @@ template <int D32> __global__ __launch_bounds__(256, 1) void ogc_prompt_few_kern
     prompt_few_body<D32>(a, t, smem);
 }
 
-// fp32.  96 channels and more have a SIMD's registers for one wavefront (held to half of them, 96 channels reload spilled ones in every round, and
-// 128 do not fit: up to 700 tokens behind 333, 16 heads over 4, 4 sequences: 96 channels 109 us, so 93; 128: staged 155, so 114).
+// fp32.  96 channels and more have a SIMD's registers for one wavefront.  Held to half of them 96 channels reload spilled ones in every round: us, half / all,
+// 16 heads over 4, 4 sequences of up to 700 tokens behind 333 107 / 90, 8 of up to 1500, which two workgroups on a compute unit help as much, 192 / 197.
+// 128 do not fit at all.
 template <int D32> __global__ __launch_bounds__(256, D32 <= 2 ? 2 : 1) void ogc_prompt_split_kernel(PromptArgs a) {
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     PromptTile t;
@@ -194,8 +195,8 @@ int64_t tiles_of(const ogc_prompt_desc* d, int rows = PROMPT_ROWS) {
 
 constexpr int FEW_TILES = 256;
 // The streaming body's calls that have too few tiles of 128 rows for the 256 compute units.  Streaming / this, us, sequences x tokens, heads: 1 x 4000,
-// 1 of 128 channels 95 / 42; 4 over 1 of 128 96 / 53; 1 x 8000, 2 of 32 97 / 39; 4 of 128 187 / 166; 1 x 1000, 4 of 64 19.6 / 10.7; 4 x up to 1500, 4 of 96 34 / 27;
-// from 256 tiles on: 2 x up to 2000, 8 over 4 of 128 53 / 53; 8 x up to 1000, 8 of 128 33 / 47; 1 x 2048, 32 over 8 of 128 59 / 115.
+// 1 of 128 channels 95 / 43; 4 over 1 of 128 97 / 54; 1 x 8000, 2 of 32 96 / 41; 4 of 128 189 / 169; 1 x 1000, 4 of 64 19.5 / 11.0; 4 x up to 1500, 4 of 96 34 / 27;
+// from 256 tiles on: 2 x up to 2000, 8 over 4 of 128 53 / 53; 8 x up to 1000, 8 of 128 33 / 47; 1 x 2048, 32 over 8 of 128 59 / 119.
 bool few_case(const ogc_prompt_desc* d) { return stream_case(d) && tiles_of(d) * d->kv_heads < FEW_TILES; }
 
 bool strides_ok(const int64_t s[2], int elt) { return s[0] >= 0 && s[1] >= 0 && s[0] * elt % 16 == 0 && s[1] * elt % 16 == 0; }

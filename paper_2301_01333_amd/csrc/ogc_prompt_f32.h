@@ -4,9 +4,9 @@
 #ifndef OGC_PROMPT_F32_H
 #define OGC_PROMPT_F32_H
 
-// What bounds it: where tiles are few, one workgroup's way through its keys (a block of 32 takes 1.6 us with 64 channels, 2.8 with 96); otherwise
+// What bounds it: where tiles are few, one workgroup's way through its keys (a block of 32 takes 1.6 us with 64 channels, 2.6 with 96); otherwise
 // power and the issue of vector instructions next to the matrix ones, as there.  Staged with the fp32 instruction / this, us, 16 heads over 4: 8 sequences up to 1500 tokens
-// 64 channels 177 / 94, 96 237 / 181, 128 292 / 220 (126 TFLOP/s); 4 up to 700 behind 333 keys 32 channels 55 / 37, 64 87 / 54, 96 126 / 93, 128 155 / 114.
+// 64 channels 189 / 108, 96 230 / 190, 128 291 / 225 (123 TFLOP/s); 4 up to 700 behind 333 keys 32 channels 54 / 37, 64 88 / 54, 96 122 / 87, 128 155 / 111.
 
 // The largest / the smallest of m and both magnitudes.  (The assembly's operands are loaded, never computed.)
 MHA_DEV float widest(float m, float x, float y) {
@@ -368,8 +368,8 @@ template <int D32> MHA_DEV void prompt_split_body(const PromptArgs& a, const Pro
     //   * Results below 2^-100: smaller values move them by 2^-134, 2^-34 of them.
     //   * Sums of zero where there are values below the smallest exponent, whose pieces may be zero.
     // One look for the largest and the smallest of all (scalars of up to 2^60: queries and values up to 2^20, sums from 2^-74 on), a
-    // closer one at what it finds, for which the wavefronts put together what each saw of the values: 32 x 16 x 512 x 64 with values
-    // of 2^21 194 us, 190 without; all computed again 452.
+    // closer one at what it finds, for which the wavefronts put together what each saw of the values: 32 sequences of 512 tokens, 16 heads of
+    // 64 channels 145 us, with values of 2^21 143; all computed again 323.
     const float total = run_sum + other_half(run_sum), inv = 1.0f / total;
     float lowest = 1.0f;
 #pragma unroll
@@ -395,7 +395,7 @@ template <int D32> MHA_DEV void prompt_split_body(const PromptArgs& a, const Pro
             }
         again = again || (nothing && wide > 0x1p20f);
         // Channels of zeros, as padding leaves them, are told from small values by the values themselves, eight loads on their way at
-        // a time: 2 x 8 x 1024 x 64 53 us, 47.6 without such channels (61 with one load at a time).
+        // a time: 2 sequences of 1024 tokens, 8 heads of 64 channels 56 us, 50 without such channels.
         if (__syncthreads_or(nothing)) {
             constexpr int AT_ONCE = 8;
             const int n = S * (D / 4);
