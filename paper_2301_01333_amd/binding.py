@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libogc_mlp.so (include/ogc_mlp.h, ogc_mha.h, ogc_decoder.h): argument marshalling only.
+"""Thin ctypes binding of libogc_mlp.so (include/ogc_mlp.h, ogc_mha.h, ogc_decoder.h, ogc_mx.h, ogc_sample.h): argument marshalling only.
 
 Every step of the path runs in the library's HIP kernels.  PyTorch appears here only as the owner
 of device memory and streams.  There is no CPU fallback: if the shared library is missing, loading
@@ -17,6 +17,9 @@ OGC_MODE_AUTO, OGC_MODE_PER_LAYER, OGC_MODE_FUSED, OGC_MODE_COOP = 0, 1, 2, 3
 OGC_LAYOUT_PLAIN, OGC_LAYOUT_BLOCKED = 0, 1
 OGC_SOFTMAX_STABLE, OGC_SOFTMAX_FAST = 0, 1
 OGC_ROPE_HALF, OGC_ROPE_INTERLEAVED = 0, 1
+OGC_MX4, OGC_MX8 = 0, 1
+OGC_NORM_SAME, OGC_NORM_MX4, OGC_NORM_MX8 = 0, 1, 2
+OGC_GATE_NONE, OGC_GATE_SILU = 0, 1
 OGC_OK = 0
 DTYPES = {"f32": OGC_F32, "bf16": OGC_BF16, "i8": OGC_I8, "f8": OGC_F8}
 
@@ -34,6 +37,9 @@ EXPORTS = [
     "ogc_rope_validate", "ogc_rope_run", "ogc_kv4_validate", "ogc_kv4_cache_bytes", "ogc_kv4_write", "ogc_kv4_read",
     "ogc_kv4_attention_validate", "ogc_kv4_attention_workspace_bytes", "ogc_kv4_attention_run",
     "ogc_prompt_validate", "ogc_prompt_run", "ogc_prompt_kernel_name",
+    "ogc_mx_bytes", "ogc_norm_validate", "ogc_norm_run", "ogc_mx_validate", "ogc_mx_write", "ogc_mx_read",
+    "ogc_mx_product_validate", "ogc_mx_product_workspace_bytes", "ogc_mx_product_run", "ogc_mx_product_kernel_name",
+    "ogc_sample_validate", "ogc_sample_workspace_bytes", "ogc_sample_run",
 ]
 OGC_ERR_TIMEOUT = -8
 
@@ -94,6 +100,26 @@ class ogc_prompt_desc(ctypes.Structure):
                 ("head_dim", ctypes.c_int32), ("q_rows", ctypes.c_int32), ("k_rows", ctypes.c_int32), ("max_q", ctypes.c_int32),
                 ("max_k", ctypes.c_int32), ("scale", ctypes.c_float), ("causal", ctypes.c_int32), ("q_stride", ctypes.c_int64 * 2),
                 ("k_stride", ctypes.c_int64 * 2), ("v_stride", ctypes.c_int64 * 2), ("o_stride", ctypes.c_int64 * 2)]
+
+
+class ogc_norm_desc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("rows", ctypes.c_int32), ("channels", ctypes.c_int32), ("out", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("x_stride", ctypes.c_int64), ("residual_stride", ctypes.c_int64), ("sum_stride", ctypes.c_int64),
+                ("y_stride", ctypes.c_int64)]
+
+
+class ogc_mx_rows(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("format", ctypes.c_int32), ("rows", ctypes.c_int32), ("channels", ctypes.c_int32),
+                ("gate", ctypes.c_int32), ("stride", ctypes.c_int64)]
+
+
+class ogc_mx_product_desc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("x_format", ctypes.c_int32), ("w_format", ctypes.c_int32), ("m", ctypes.c_int32),
+                ("n", ctypes.c_int32), ("k", ctypes.c_int32), ("has_bias", ctypes.c_int32), ("y_stride", ctypes.c_int64)]
+
+
+class ogc_sample_desc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("stride", ctypes.c_int64)]
 
 
 class OgcError(RuntimeError):
@@ -191,6 +217,16 @@ def lib():
                            ("ogc_prompt_validate", [prompt]), ("ogc_prompt_run", [prompt] + 7 * [vp])):
             getattr(l, name).argtypes, getattr(l, name).restype = args, i32
         l.ogc_prompt_kernel_name.argtypes, l.ogc_prompt_kernel_name.restype = [prompt], ctypes.c_char_p
+        norm, mx, product, sample = (ctypes.POINTER(t) for t in (ogc_norm_desc, ogc_mx_rows, ogc_mx_product_desc, ogc_sample_desc))
+        size = ctypes.POINTER(sz)
+        for name, args in (("ogc_mx_bytes", [i32, i32, i32, size, size]), ("ogc_norm_validate", [norm]), ("ogc_norm_run", [norm] + 7 * [vp]),
+                           ("ogc_mx_validate", [mx]), ("ogc_mx_write", [mx] + 4 * [vp]), ("ogc_mx_read", [mx] + 4 * [vp]),
+                           ("ogc_mx_product_validate", [product]), ("ogc_mx_product_workspace_bytes", [product, size]),
+                           ("ogc_mx_product_run", [product] + 8 * [vp]),
+                           ("ogc_sample_validate", [sample]), ("ogc_sample_workspace_bytes", [sample, size]),
+                           ("ogc_sample_run", [sample] + 10 * [vp])):
+            getattr(l, name).argtypes, getattr(l, name).restype = args, i32
+        l.ogc_mx_product_kernel_name.argtypes, l.ogc_mx_product_kernel_name.restype = [product], ctypes.c_char_p
         _lib = l
     return _lib
 
@@ -499,6 +535,91 @@ def ogc_prompt_run(desc: ogc_prompt_desc, q_ptr: int, k_ptr: int, v_ptr: int, cu
 def ogc_prompt_kernel_name(desc: ogc_prompt_desc) -> str:
     r = lib().ogc_prompt_kernel_name(desc)
     return r.decode() if r else ""
+
+
+# ---- a decoder's projections in microscaled formats (include/ogc_mx.h); strides in elements
+def ogc_mx_bytes(fmt: int, rows: int, channels: int):
+    """Bytes of a microscaled matrix: (codes, scales)."""
+    codes, scales = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(lib().ogc_mx_bytes(int(fmt), int(rows), int(channels), ctypes.byref(codes), ctypes.byref(scales)), "ogc_mx_bytes")
+    return codes.value, scales.value
+
+
+def norm_desc(dtype: int, rows: int, channels: int, out: int, eps: float, x_stride: int, residual_stride: int = 0, sum_stride: int = 0,
+              y_stride: int = 0) -> ogc_norm_desc:
+    return ogc_norm_desc(int(dtype), int(rows), int(channels), int(out), float(eps), int(x_stride), int(residual_stride), int(sum_stride),
+                         int(y_stride))
+
+
+def ogc_norm_validate(desc: ogc_norm_desc) -> int:
+    return int(lib().ogc_norm_validate(desc))
+
+
+def ogc_norm_run(desc: ogc_norm_desc, x_ptr: int, residual_ptr: int, weight_ptr: int, sum_ptr: int, y_ptr: int, scales_ptr: int = 0,
+                 stream: int = 0) -> None:
+    _check(lib().ogc_norm_run(desc, x_ptr, residual_ptr, weight_ptr, sum_ptr, y_ptr, scales_ptr, stream), "ogc_norm_run")
+
+
+def mx_rows(dtype: int, fmt: int, rows: int, channels: int, gate: int, stride: int) -> ogc_mx_rows:
+    return ogc_mx_rows(int(dtype), int(fmt), int(rows), int(channels), int(gate), int(stride))
+
+
+def ogc_mx_validate(rows: ogc_mx_rows) -> int:
+    return int(lib().ogc_mx_validate(rows))
+
+
+def ogc_mx_write(rows: ogc_mx_rows, x_ptr: int, codes_ptr: int, scales_ptr: int, stream: int = 0) -> None:
+    _check(lib().ogc_mx_write(rows, x_ptr, codes_ptr, scales_ptr, stream), "ogc_mx_write")
+
+
+def ogc_mx_read(rows: ogc_mx_rows, codes_ptr: int, scales_ptr: int, y_ptr: int, stream: int = 0) -> None:
+    _check(lib().ogc_mx_read(rows, codes_ptr, scales_ptr, y_ptr, stream), "ogc_mx_read")
+
+
+def mx_product_desc(dtype: int, x_format: int, w_format: int, m: int, n: int, k: int, has_bias: int, y_stride: int) -> ogc_mx_product_desc:
+    return ogc_mx_product_desc(int(dtype), int(x_format), int(w_format), int(m), int(n), int(k), int(has_bias), int(y_stride))
+
+
+def ogc_mx_product_validate(desc: ogc_mx_product_desc) -> int:
+    return int(lib().ogc_mx_product_validate(desc))
+
+
+def ogc_mx_product_workspace_bytes(desc: ogc_mx_product_desc) -> int:
+    v = ctypes.c_size_t()
+    _check(lib().ogc_mx_product_workspace_bytes(desc, ctypes.byref(v)), "ogc_mx_product_workspace_bytes")
+    return v.value
+
+
+def ogc_mx_product_run(desc: ogc_mx_product_desc, x_ptr: int, x_scales_ptr: int, w_ptr: int, w_scales_ptr: int, bias_ptr: int, y_ptr: int,
+                       workspace_ptr: int, stream: int = 0) -> None:
+    _check(lib().ogc_mx_product_run(desc, x_ptr, x_scales_ptr, w_ptr, w_scales_ptr, bias_ptr, y_ptr, workspace_ptr, stream),
+           "ogc_mx_product_run")
+
+
+def ogc_mx_product_kernel_name(desc: ogc_mx_product_desc) -> str:
+    r = lib().ogc_mx_product_kernel_name(desc)
+    return r.decode() if r else ""
+
+
+# ---- the choice of a token (include/ogc_sample.h)
+def sample_desc(dtype: int, rows: int, vocab: int, stride: int) -> ogc_sample_desc:
+    return ogc_sample_desc(int(dtype), int(rows), int(vocab), int(stride))
+
+
+def ogc_sample_validate(desc: ogc_sample_desc) -> int:
+    return int(lib().ogc_sample_validate(desc))
+
+
+def ogc_sample_workspace_bytes(desc: ogc_sample_desc) -> int:
+    v = ctypes.c_size_t()
+    _check(lib().ogc_sample_workspace_bytes(desc, ctypes.byref(v)), "ogc_sample_workspace_bytes")
+    return v.value
+
+
+def ogc_sample_run(desc: ogc_sample_desc, logits_ptr: int, temperature_ptr: int, top_k_ptr: int, top_p_ptr: int, min_p_ptr: int,
+                   uniform_ptr: int, tokens_ptr: int, log_probabilities_ptr: int, workspace_ptr: int, stream: int = 0) -> None:
+    _check(lib().ogc_sample_run(desc, logits_ptr, temperature_ptr, top_k_ptr, top_p_ptr, min_p_ptr, uniform_ptr, tokens_ptr,
+                                log_probabilities_ptr, workspace_ptr, stream), "ogc_sample_run")
 
 
 # ---- convenience wrapper: owns the torch tensors the library needs ---------------------------------

@@ -1,0 +1,166 @@
+// The product of microscaled rows with microscaled weights (include/ogc_mx.h).
+#include "ogc_mx_rows.h"
+
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+
+struct ProductArgs {
+    const uint8_t* x;
+    const uint8_t* xs;
+    const uint8_t* w;
+    const uint8_t* ws;
+    const float* bias;  // or NULL
+    uint8_t* y;
+    long long sy;  // bytes
+    int m, n, padded;
+    int steps;  // of 256 channels
+};
+
+// One operand of one instruction: 64 channels of 32 rows, which lie in memory as its lanes take them.
+template <int FORMAT> struct Operand {
+    v4i part[FORMAT == OGC_MX8 ? 2 : 1];
+    __device__ __forceinline__ void load(const uint8_t* p) {
+        part[0] = *(const v4i*)p;
+        if constexpr (FORMAT == OGC_MX8) part[1] = *(const v4i*)(p + 1024);
+    }
+    __device__ __forceinline__ v8i whole() const {
+        if constexpr (FORMAT == OGC_MX8) return __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
+        else return __builtin_shufflevector(part[0], part[0], 0, 1, 2, 3, -1, -1, -1, -1);
+    }
+    static constexpr int BYTES = FORMAT == OGC_MX8 ? 2048 : 1024;
+};
+// c += w x, both of 64 channels; I: which quarter of 256 channels, and so which byte of the scales
+template <int XF, int I> MX_DEV v16f product(const Operand<OGC_MX4>& w, const Operand<XF>& x, v16f c, uint32_t ws, uint32_t xs) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w.whole(), x.whole(), c, 4, XF == OGC_MX8 ? 0 : 4, I, (int)ws, I, (int)xs);
+}
+
+// y's rows row .. of four channels n0 .. from their sums; `n0` is a multiple of four
+template <int DT> MX_DEV void put4(const ProductArgs& a, int row, int n0, v4f v) {
+    if (row >= a.m || n0 >= a.n) return;
+    const int there = a.n - n0;
+    if (a.bias) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < there) v[i] += a.bias[n0 + i];
+    }
+    uint8_t* const p = a.y + row * a.sy + (int64_t)n0 * (DT == OGC_F32 ? 4 : 2);
+    if constexpr (DT == OGC_F32) {
+        if (there >= 4) *(v4f*)p = v;
+        else
+            for (int i = 0; i < there; ++i) ((float*)p)[i] = v[i];
+    } else {
+        const mx_v2bf lo = {(__bf16)v[0], (__bf16)v[1]}, hi = {(__bf16)v[2], (__bf16)v[3]};
+        const mx_v2u r = {__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+        if (there >= 4) *(mx_v2u*)p = r;
+        else
+            for (int i = 0; i < there; ++i) ((uint16_t*)p)[i] = (uint16_t)(r[i / 2] >> (i % 2 * 16));
+    }
+}
+
+constexpr int FEW_WAVES = 4;
+
+// A workgroup has 32 rows and 32 weights; its wavefronts take the channels in turn, 256 at a time, straight from memory, and add up in LDS.
+template <int DT, int XF> __global__ __launch_bounds__(64 * FEW_WAVES) void ogc_mx_few_kernel(ProductArgs a) {
+    constexpr int PITCH = 36;  // floats of a row's 32 sums: the 16-byte pieces of eight rows are on distinct banks
+    __shared__ __attribute__((aligned(16))) float sums[FEW_WAVES][32 * PITCH];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n0 = blockIdx.x, m0 = blockIdx.y;  // in blocks of 32
+    const uint8_t* w = a.w + n0 * mx_codes_of_32(OGC_MX4, a.padded) + lane * 16;
+    const uint8_t* x = a.x + m0 * mx_codes_of_32(XF, a.padded) + lane * 16;
+    const uint8_t* ws = a.ws + (int64_t)n0 * a.padded + lane * 4;
+    const uint8_t* xs = a.xs + (int64_t)m0 * a.padded + lane * 4;
+    v16f c;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) c[i] = 0.0f;
+    for (int s = wave; s < a.steps; s += FEW_WAVES) {
+        Operand<OGC_MX4> p[4];
+        Operand<XF> q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            p[i].load(w + ((int64_t)s * 4 + i) * Operand<OGC_MX4>::BYTES);
+            q[i].load(x + ((int64_t)s * 4 + i) * Operand<XF>::BYTES);
+        }
+        const uint32_t u = *(const uint32_t*)(ws + (int64_t)s * 256), v = *(const uint32_t*)(xs + (int64_t)s * 256);
+        c = product<XF, 0>(p[0], q[0], c, u, v);
+        c = product<XF, 1>(p[1], q[1], c, u, v);
+        c = product<XF, 2>(p[2], q[2], c, u, v);
+        c = product<XF, 3>(p[3], q[3], c, u, v);
+    }
+    // lane l has the weights 8 q + 4 (l / 32) .. of row l % 32 in its registers 4 q ..
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        *(v4f*)(&sums[wave][lane % 32 * PITCH + q * 8 + lane / 32 * 4]) = (v4f){c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
+    __syncthreads();
+    const int row = threadIdx.x / 8, at = threadIdx.x % 8 * 4;
+    v4f v = *(const v4f*)(&sums[0][row * PITCH + at]);
+#pragma unroll
+    for (int i = 1; i < FEW_WAVES; ++i) v += *(const v4f*)(&sums[i][row * PITCH + at]);
+    put4<DT>(a, m0 * 32 + row, n0 * 32 + at, v);
+}
+
+extern "C" {
+
+ogc_status ogc_mx_product_validate(const ogc_mx_product_desc* d) {
+    if (!d) return OGC_ERR_INVALID_ARG;
+    if (d->dtype < OGC_F32 || d->dtype > OGC_F8) return OGC_ERR_INVALID_ARG;
+    for (int32_t f : {d->x_format, d->w_format})
+        if (f != OGC_MX4 && f != OGC_MX8) return OGC_ERR_INVALID_ARG;
+    if (d->has_bias != 0 && d->has_bias != 1) return OGC_ERR_INVALID_ARG;
+    if (d->m < 0 || d->n <= 0 || d->k <= 0 || d->k > 1 << 20) return OGC_ERR_SHAPE;
+    if (d->m > 65535 * 32 || d->n > 32 * 0xffffff / 8) return OGC_ERR_SHAPE;  // blocks of a launch
+    if (d->w_format != OGC_MX4 || (d->dtype != OGC_F32 && d->dtype != OGC_BF16)) return OGC_ERR_UNSUPPORTED;
+    if (d->y_stride < 0 || d->y_stride * (d->dtype == OGC_F32 ? 4 : 2) % 16 != 0) return OGC_ERR_ALIGNMENT;
+    return OGC_OK;
+}
+
+ogc_status ogc_mx_product_workspace_bytes(const ogc_mx_product_desc* d, size_t* bytes) {
+    const ogc_status st = ogc_mx_product_validate(d);
+    if (st != OGC_OK) return st;
+    if (!bytes) return OGC_ERR_INVALID_ARG;
+    *bytes = 0;
+    return OGC_OK;
+}
+
+const char* ogc_mx_product_kernel_name(const ogc_mx_product_desc* d) {
+    if (ogc_mx_product_validate(d) != OGC_OK) return nullptr;
+    static const char* const names[2][2] = {{"ogc_mx_few_kernel<0, 0>", "ogc_mx_few_kernel<0, 1>"}, {"ogc_mx_few_kernel<1, 0>", "ogc_mx_few_kernel<1, 1>"}};
+    return names[d->dtype][d->x_format];
+}
+
+ogc_status ogc_mx_product_run(const ogc_mx_product_desc* d, const void* x, const void* x_scales, const void* w, const void* w_scales,
+                              const float* bias, void* y, void* workspace, void* stream) {
+    const ogc_status st = ogc_mx_product_validate(d);
+    if (st != OGC_OK) return st;
+    if (d->m == 0) return OGC_OK;
+    if (!x || !x_scales || !w || !w_scales || !y || (d->has_bias && !bias)) return OGC_ERR_INVALID_ARG;
+    if (((uintptr_t)x | (uintptr_t)x_scales | (uintptr_t)w | (uintptr_t)w_scales | (uintptr_t)y) & 15) return OGC_ERR_ALIGNMENT;
+    if (d->has_bias && ((uintptr_t)bias & 3)) return OGC_ERR_ALIGNMENT;
+    (void)workspace;
+    ProductArgs a;
+    a.x = (const uint8_t*)x;
+    a.xs = (const uint8_t*)x_scales;
+    a.w = (const uint8_t*)w;
+    a.ws = (const uint8_t*)w_scales;
+    a.bias = d->has_bias ? bias : nullptr;
+    a.y = (uint8_t*)y;
+    a.sy = d->y_stride * (d->dtype == OGC_F32 ? 4 : 2);
+    a.m = d->m;
+    a.n = d->n;
+    a.padded = mx_padded_channels(d->k);
+    a.steps = a.padded / MX_BLOCK;
+    const hipStream_t s = (hipStream_t)stream;
+    const dim3 grid((unsigned)((d->n + 31) / 32), (unsigned)((d->m + 31) / 32)), threads(64 * FEW_WAVES);
+    const bool eight = d->x_format == OGC_MX8;
+    if (d->dtype == OGC_F32) {
+        if (eight) hipLaunchKernelGGL((ogc_mx_few_kernel<OGC_F32, OGC_MX8>), grid, threads, 0, s, a);
+        else hipLaunchKernelGGL((ogc_mx_few_kernel<OGC_F32, OGC_MX4>), grid, threads, 0, s, a);
+    } else {
+        if (eight) hipLaunchKernelGGL((ogc_mx_few_kernel<OGC_BF16, OGC_MX8>), grid, threads, 0, s, a);
+        else hipLaunchKernelGGL((ogc_mx_few_kernel<OGC_BF16, OGC_MX4>), grid, threads, 0, s, a);
+    }
+    return hipGetLastError() == hipSuccess ? OGC_OK : OGC_ERR_DEVICE;
+}
+
+}  // extern "C"

@@ -1,0 +1,212 @@
+// The residual's addition with the root-mean-square norm (include/ogc_mx.h): rows in their own type or in a microscaled format.
+//
+// Rows are read once, kept in registers, and written twice (the sum and its norm): the kernel is bound by memory, or by its launch.  A
+// lane holds N runs of eight channels.  In its own type a workgroup has one row; in a microscaled format it has eight, eight lanes of a
+// wavefront each, because the codes of eight rows are 128 bytes side by side in the matrix, and a wavefront's four runs of a row
+// are a block of 256 channels, whose four scales are one word.  Rows that do not fit the registers (N = 0) are read a second time for the norm.
+#include "ogc_mx_rows.h"
+
+#include <math.h>
+
+namespace {
+
+struct NormArgs {
+    const uint8_t* x;
+    const uint8_t* residual;  // or NULL
+    const float* weight;
+    uint8_t* sum;
+    uint8_t* y;  // rows, or codes
+    uint8_t* scales;
+    long long sx, sr, ss, sy;  // bytes
+    int rows, channels, padded;
+    float eps, inv;  // inv: 1 / channels
+};
+
+constexpr int NORM_WAVES = 16;
+
+template <int DT, int OUT, int N> __global__ __launch_bounds__(64 * NORM_WAVES) void ogc_norm_kernel(NormArgs a) {
+    constexpr int E = MxEight<DT>::E, ROWS = OUT == OGC_NORM_SAME ? 1 : 8, LANES = 64 / ROWS;  // rows of a workgroup, lanes of a row in a wavefront
+    __shared__ float part[NORM_WAVES][ROWS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + lane / LANES;
+    const int j = lane % LANES;
+    const bool on = row < a.rows;
+    const int64_t r = on ? row : 0;
+    const uint8_t *const x = a.x + r * a.sx, *const res = a.residual ? a.residual + r * a.sr : nullptr;
+    uint8_t* const sum = a.residual ? a.sum + r * a.ss : nullptr;
+    // first channel of a lane's run i: whole wavefronts of a row take 512 channels in turn, those of eight rows 256
+    const auto first = [&](int i) {
+        return OUT == OGC_NORM_SAME ? (i * waves + wave) * 512 + j * 8 : (i / 4 * waves + wave) * MX_BLOCK + i % 4 * 64 + j * 8;
+    };
+    const int limit = OUT == OGC_NORM_SAME ? a.channels : a.padded;
+    const int runs = OUT == OGC_NORM_SAME ? (limit + 512 * waves - 1) / (512 * waves) : (limit + MX_BLOCK * waves - 1) / (MX_BLOCK * waves) * 4;
+
+    MxEight<DT> held[N > 0 ? N : 1];
+    float square = 0.0f;
+    const auto take = [&](MxEight<DT>& s, const MxEight<DT>& more, int c) {
+        const int there = on ? a.channels - c : 0;
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = res ? s.get(i) + more.get(i) : s.get(i);
+        if (res) {
+            s.set(v);  // (rounded: the norm is the norm of what the next layer adds to)
+            if (there > 0) s.store(sum + (int64_t)c * E, there);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) square = __builtin_fmaf(s.get(i), s.get(i), square);
+    };
+    if constexpr (N > 0) {
+        constexpr int M = DT == OGC_F32 && N > 4 ? 4 : N;  // (registers: eight runs of fp32 have their residuals four at a time)
+#pragma unroll
+        for (int i0 = 0; i0 < N; i0 += M) {
+            MxEight<DT> more[M];
+#pragma unroll
+            for (int i = 0; i < M; ++i) {
+                const int c = first(i0 + i), there = on ? a.channels - c : 0;
+                held[i0 + i].load(x + (int64_t)c * E, there);
+                if (res) more[i].load(res + (int64_t)c * E, there);
+                else more[i].clear();
+            }
+#pragma unroll
+            for (int i = 0; i < M; ++i) take(held[i0 + i], more[i], first(i0 + i));
+        }
+    } else {
+        for (int i = 0; i < runs; ++i) {
+            const int c = first(i), there = on ? a.channels - c : 0;
+            MxEight<DT> s, more;
+            s.load(x + (int64_t)c * E, there);
+            if (res) more.load(res + (int64_t)c * E, there);
+            else more.clear();
+            take(s, more, c);
+        }
+    }
+#pragma unroll
+    for (int m = 1; m < LANES; m *= 2) square += __shfl_xor(square, m);
+    if (waves > 1) {
+        if (j == 0) part[wave][lane / LANES] = square;
+        __syncthreads();
+        square = 0.0f;
+        for (int w = 0; w < waves; ++w) square += part[w][lane / LANES];
+    }
+    const float f = 1.0f / __builtin_sqrtf(square * a.inv + a.eps);
+
+    const auto give = [&](const MxEight<DT>& s, int c, uint32_t& scales, int i) {
+        const int there = on ? a.channels - c : 0;
+        float v[8];
+        if (there >= 8) {
+            const mx_v4f w0 = *(const mx_v4f*)(a.weight + c), w1 = *(const mx_v4f*)(a.weight + c + 4);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = s.get(k) * f * (k < 4 ? w0[k % 4] : w1[k % 4]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = k < there ? s.get(k) * f * a.weight[c + k] : 0.0f;
+        }
+        if constexpr (OUT == OGC_NORM_SAME) {
+            MxEight<DT> y;
+            y.set(v);
+            if (there > 0) y.store(a.y + r * a.sy + (int64_t)c * E, there);
+        } else {
+            constexpr int FORMAT = OUT == OGC_NORM_MX8 ? OGC_MX8 : OGC_MX4;
+            uint32_t e;
+            const mx_v2u code = mx_quantized<FORMAT>(v, e);
+            scales = i % 4 ? scales | e << (i % 4 * 8) : e;
+            if (on && c < a.padded) {
+                uint8_t* const o = a.y + mx_code_at(FORMAT, a.padded, (int)row, c);
+                if constexpr (FORMAT == OGC_MX8) *(mx_v2u*)o = code;
+                else *(uint32_t*)o = code[0];
+                if (i % 4 == 3 && j % 4 == 0) *(uint32_t*)(a.scales + mx_scales_at(a.padded, (int)row, c / MX_BLOCK, j / 4)) = scales;
+            }
+        }
+    };
+    uint32_t scales = 0;
+    if constexpr (N > 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) give(held[i], first(i), scales, i);
+    } else {
+        const uint8_t* const again = res ? sum : x;  // (a lane reads what it wrote itself)
+        for (int i = 0; i < runs; ++i) {
+            const int c = first(i);
+            MxEight<DT> s;
+            s.load(again + (int64_t)c * E, on ? a.channels - c : 0);
+            give(s, c, scales, i);
+        }
+    }
+}
+
+template <int DT, int OUT> void launch(const NormArgs& a, hipStream_t st) {
+    constexpr int ROWS = OUT == OGC_NORM_SAME ? 1 : 8, SPAN = OUT == OGC_NORM_SAME ? 512 : 256, RUNS = OUT == OGC_NORM_SAME ? 1 : 4;  // channels and runs of a wavefront's turn
+    const unsigned grid = (unsigned)(((int64_t)a.rows + ROWS - 1) / ROWS);
+    const int turns = ((OUT == OGC_NORM_SAME ? a.channels : a.padded) + SPAN - 1) / SPAN;
+    int waves = 1;
+    while (waves < NORM_WAVES && turns > waves * (8 / RUNS)) waves *= 2;
+    if (grid < 1024)
+        while (waves < NORM_WAVES && turns > waves) waves *= 2;
+    const int runs = (turns + waves - 1) / waves * RUNS;
+    const dim3 g(grid), t(64 * waves);
+    if constexpr (RUNS == 1) {
+        if (runs <= 2) {
+            if (runs <= 1) hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, 1>), g, t, 0, st, a);
+            else hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, 2>), g, t, 0, st, a);
+            return;
+        }
+    }
+    if (runs <= 4) hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, 4>), g, t, 0, st, a);
+    else if (runs <= 8) hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, 8>), g, t, 0, st, a);
+    else hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, 0>), g, t, 0, st, a);
+}
+
+bool aligned(int64_t stride, int e) { return stride >= 0 && stride * e % 16 == 0; }
+
+}  // namespace
+
+extern "C" {
+
+ogc_status ogc_norm_validate(const ogc_norm_desc* d) {
+    if (!d) return OGC_ERR_INVALID_ARG;
+    if (d->dtype < OGC_F32 || d->dtype > OGC_F8 || d->out < OGC_NORM_SAME || d->out > OGC_NORM_MX8) return OGC_ERR_INVALID_ARG;
+    if (!(d->eps >= 0.0f && isfinite(d->eps))) return OGC_ERR_INVALID_ARG;
+    if (d->rows < 0 || d->channels <= 0 || d->channels > 1 << 20) return OGC_ERR_SHAPE;
+    if (d->rows > 0x3fffff) return OGC_ERR_SHAPE;  // a workgroup of up to 1024 threads for each: a grid of fewer than 2^32
+    if (d->dtype != OGC_F32 && d->dtype != OGC_BF16) return OGC_ERR_UNSUPPORTED;
+    const int e = d->dtype == OGC_F32 ? 4 : 2;
+    if (!aligned(d->x_stride, e) || !aligned(d->residual_stride, e) || !aligned(d->sum_stride, e)) return OGC_ERR_ALIGNMENT;
+    if (d->out == OGC_NORM_SAME && !aligned(d->y_stride, e)) return OGC_ERR_ALIGNMENT;
+    return OGC_OK;
+}
+
+ogc_status ogc_norm_run(const ogc_norm_desc* d, const void* x, const void* residual, const float* weight, void* sum, void* y,
+                        void* scales, void* stream) {
+    const ogc_status st = ogc_norm_validate(d);
+    if (st != OGC_OK) return st;
+    if (d->rows == 0) return OGC_OK;
+    const bool same = d->out == OGC_NORM_SAME;
+    if (!x || !weight || !y || (residual && !sum) || (!same && !scales)) return OGC_ERR_INVALID_ARG;
+    if (((uintptr_t)x | (uintptr_t)weight | (uintptr_t)y) & 15) return OGC_ERR_ALIGNMENT;
+    if (residual && (((uintptr_t)residual | (uintptr_t)sum) & 15)) return OGC_ERR_ALIGNMENT;
+    if (!same && ((uintptr_t)scales & 15)) return OGC_ERR_ALIGNMENT;
+    const int e = d->dtype == OGC_F32 ? 4 : 2;
+    NormArgs a;
+    a.x = (const uint8_t*)x;
+    a.residual = (const uint8_t*)residual;
+    a.weight = weight;
+    a.sum = (uint8_t*)sum;
+    a.y = (uint8_t*)y;
+    a.scales = (uint8_t*)scales;
+    a.sx = d->x_stride * e;
+    a.sr = d->residual_stride * e;
+    a.ss = d->sum_stride * e;
+    a.sy = d->y_stride * e;
+    a.rows = d->rows;
+    a.channels = d->channels;
+    a.padded = mx_padded_channels(d->channels);
+    a.eps = d->eps;
+    a.inv = 1.0f / (float)d->channels;
+    const hipStream_t s = (hipStream_t)stream;
+    const bool f32 = d->dtype == OGC_F32;
+    if (same) f32 ? launch<OGC_F32, OGC_NORM_SAME>(a, s) : launch<OGC_BF16, OGC_NORM_SAME>(a, s);
+    else if (d->out == OGC_NORM_MX4) f32 ? launch<OGC_F32, OGC_NORM_MX4>(a, s) : launch<OGC_BF16, OGC_NORM_MX4>(a, s);
+    else f32 ? launch<OGC_F32, OGC_NORM_MX8>(a, s) : launch<OGC_BF16, OGC_NORM_MX8>(a, s);
+    return hipGetLastError() == hipSuccess ? OGC_OK : OGC_ERR_DEVICE;
+}
+
+}  // extern "C"
