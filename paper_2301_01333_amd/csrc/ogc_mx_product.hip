@@ -1,5 +1,8 @@
 // The product of microscaled rows with microscaled weights (include/ogc_mx.h).
+#include "ogc_lds_limit.h"
 #include "ogc_mx_rows.h"
+
+#include <type_traits>
 
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v8i __attribute__((ext_vector_type(8)));
@@ -16,6 +19,7 @@ struct ProductArgs {
     long long sy;  // bytes
     int m, n, padded;
     int steps;  // of 256 channels
+    int tiles_n, tiles_m;
 };
 
 // One operand of one instruction: 64 channels of 32 rows, which lie in memory as its lanes take them.
@@ -36,26 +40,26 @@ template <int XF, int I> MX_DEV v16f product(const Operand<OGC_MX4>& w, const Op
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w.whole(), x.whole(), c, 4, XF == OGC_MX8 ? 0 : 4, I, (int)ws, I, (int)xs);
 }
 
-// y's rows row .. of four channels n0 .. from their sums; `n0` is a multiple of four
-template <int DT> MX_DEV void put4(const ProductArgs& a, int row, int n0, v4f v) {
-    if (row >= a.m || n0 >= a.n) return;
-    const int there = a.n - n0;
-    if (a.bias) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < there) v[i] += a.bias[n0 + i];
-    }
-    uint8_t* const p = a.y + row * a.sy + (int64_t)n0 * (DT == OGC_F32 ? 4 : 2);
-    if constexpr (DT == OGC_F32) {
-        if (there >= 4) *(v4f*)p = v;
-        else
-            for (int i = 0; i < there; ++i) ((float*)p)[i] = v[i];
-    } else {
+// four channels of a row of y, rounded once
+template <int DT> MX_DEV void put4_whole(uint8_t* p, v4f v) {
+    if constexpr (DT == OGC_F32) *(v4f*)p = v;
+    else {
         const mx_v2bf lo = {(__bf16)v[0], (__bf16)v[1]}, hi = {(__bf16)v[2], (__bf16)v[3]};
-        const mx_v2u r = {__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
-        if (there >= 4) *(mx_v2u*)p = r;
-        else
-            for (int i = 0; i < there; ++i) ((uint16_t*)p)[i] = (uint16_t)(r[i / 2] >> (i % 2 * 16));
+        *(mx_v2u*)p = (mx_v2u){__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+    }
+}
+// the same where there may be fewer of them, or none; n0 is a multiple of four
+template <int DT> MX_DEV void put4(const ProductArgs& a, int row, int n0, v4f v) {
+    const int there = row < a.m ? a.n - n0 : 0;
+    uint8_t* const p = a.y + row * a.sy + (int64_t)n0 * (DT == OGC_F32 ? 4 : 2);
+    if (there >= 4) put4_whole<DT>(p, v);
+    else if (there > 0) {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < there) {
+                if constexpr (DT == OGC_F32) ((float*)p)[i] = v[i];
+                else ((__bf16*)p)[i] = (__bf16)v[i];
+            }
     }
 }
 
@@ -97,8 +101,47 @@ template <int DT, int XF> __global__ __launch_bounds__(64 * FEW_WAVES) void ogc_
     v4f v = *(const v4f*)(&sums[0][row * PITCH + at]);
 #pragma unroll
     for (int i = 1; i < FEW_WAVES; ++i) v += *(const v4f*)(&sums[i][row * PITCH + at]);
+    if (a.bias) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += n0 * 32 + at + i < a.n ? a.bias[n0 * 32 + at + i] : 0.0f;
+    }
     put4<DT>(a, m0 * 32 + row, n0 * 32 + at, v);
 }
+
+#include "ogc_mx_tile.h"
+
+namespace {
+
+// Which kernel a call takes, and how many workgroups: the same for its launch and its name.
+enum { FEW, TILE_128, TILE_256 };
+int kernel_for(const ogc_mx_product_desc* d) {
+    const int64_t tiles = ((int64_t)d->n + 255) / 256 * (((int64_t)d->m + 255) / 256);
+    if (d->m <= 32) return FEW;
+    return tiles >= 128 ? TILE_256 : TILE_128;
+}
+
+template <int DT, int XF, int WN, int WM, int NB, int MB> bool launch_tiles(ProductArgs a, hipStream_t s) {
+    typedef MxTile<XF, WN, WM, NB, MB> T;
+    static OgcLdsLimit limit;
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess) return false;
+    const void* const kern = (const void*)ogc_mx_tile_kernel<DT, XF, WN, WM, NB, MB>;
+    if (limit.raise(dev, T::LDS, [&]() { return (int)hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS); }) != 0) return false;
+    a.tiles_n = (a.n + T::TN * 32 - 1) / (T::TN * 32);
+    a.tiles_m = (a.m + T::TM * 32 - 1) / (T::TM * 32);
+    const unsigned grid = (unsigned)(((int64_t)a.tiles_n * a.tiles_m + 7) / 8 * 8);
+    hipLaunchKernelGGL((ogc_mx_tile_kernel<DT, XF, WN, WM, NB, MB>), dim3(grid), dim3(64 * T::WAVES), T::LDS, s, a);
+    return true;
+}
+template <int DT, int XF> bool launch(int which, const ProductArgs& a, hipStream_t s) {
+    if (which == TILE_256) return launch_tiles<DT, XF, 2, 4, 4, 2>(a, s);
+    if (which == TILE_128) return launch_tiles<DT, XF, 2, 2, 2, 2>(a, s);
+    const dim3 grid((unsigned)((a.n + 31) / 32), (unsigned)((a.m + 31) / 32));
+    hipLaunchKernelGGL((ogc_mx_few_kernel<DT, XF>), grid, dim3(64 * FEW_WAVES), 0, s, a);
+    return true;
+}
+
+}  // namespace
 
 extern "C" {
 
@@ -125,8 +168,11 @@ ogc_status ogc_mx_product_workspace_bytes(const ogc_mx_product_desc* d, size_t* 
 
 const char* ogc_mx_product_kernel_name(const ogc_mx_product_desc* d) {
     if (ogc_mx_product_validate(d) != OGC_OK) return nullptr;
-    static const char* const names[2][2] = {{"ogc_mx_few_kernel<0, 0>", "ogc_mx_few_kernel<0, 1>"}, {"ogc_mx_few_kernel<1, 0>", "ogc_mx_few_kernel<1, 1>"}};
-    return names[d->dtype][d->x_format];
+    static const char* const names[3][2][2] = {
+        {{"ogc_mx_few_kernel<0, 0>", "ogc_mx_few_kernel<0, 1>"}, {"ogc_mx_few_kernel<1, 0>", "ogc_mx_few_kernel<1, 1>"}},
+        {{"ogc_mx_tile_kernel<0, 0, 2, 2, 2, 2>", "ogc_mx_tile_kernel<0, 1, 2, 2, 2, 2>"}, {"ogc_mx_tile_kernel<1, 0, 2, 2, 2, 2>", "ogc_mx_tile_kernel<1, 1, 2, 2, 2, 2>"}},
+        {{"ogc_mx_tile_kernel<0, 0, 2, 4, 4, 2>", "ogc_mx_tile_kernel<0, 1, 2, 4, 4, 2>"}, {"ogc_mx_tile_kernel<1, 0, 2, 4, 4, 2>", "ogc_mx_tile_kernel<1, 1, 2, 4, 4, 2>"}}};
+    return names[kernel_for(d)][d->dtype][d->x_format];
 }
 
 ogc_status ogc_mx_product_run(const ogc_mx_product_desc* d, const void* x, const void* x_scales, const void* w, const void* w_scales,
@@ -151,15 +197,12 @@ ogc_status ogc_mx_product_run(const ogc_mx_product_desc* d, const void* x, const
     a.padded = mx_padded_channels(d->k);
     a.steps = a.padded / MX_BLOCK;
     const hipStream_t s = (hipStream_t)stream;
-    const dim3 grid((unsigned)((d->n + 31) / 32), (unsigned)((d->m + 31) / 32)), threads(64 * FEW_WAVES);
+    a.tiles_n = a.tiles_m = 0;
     const bool eight = d->x_format == OGC_MX8;
-    if (d->dtype == OGC_F32) {
-        if (eight) hipLaunchKernelGGL((ogc_mx_few_kernel<OGC_F32, OGC_MX8>), grid, threads, 0, s, a);
-        else hipLaunchKernelGGL((ogc_mx_few_kernel<OGC_F32, OGC_MX4>), grid, threads, 0, s, a);
-    } else {
-        if (eight) hipLaunchKernelGGL((ogc_mx_few_kernel<OGC_BF16, OGC_MX8>), grid, threads, 0, s, a);
-        else hipLaunchKernelGGL((ogc_mx_few_kernel<OGC_BF16, OGC_MX4>), grid, threads, 0, s, a);
-    }
+    const int which = kernel_for(d);
+    const bool sent = d->dtype == OGC_F32 ? (eight ? launch<OGC_F32, OGC_MX8>(which, a, s) : launch<OGC_F32, OGC_MX4>(which, a, s))
+                                          : (eight ? launch<OGC_BF16, OGC_MX8>(which, a, s) : launch<OGC_BF16, OGC_MX4>(which, a, s));
+    if (!sent) return OGC_ERR_DEVICE;
     return hipGetLastError() == hipSuccess ? OGC_OK : OGC_ERR_DEVICE;
 }
 

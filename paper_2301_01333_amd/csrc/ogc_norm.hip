@@ -19,14 +19,15 @@ struct NormArgs {
     uint8_t* scales;
     long long sx, sr, ss, sy;  // bytes
     int rows, channels, padded;
-    float eps, inv;  // inv: 1 / channels
+    float eps;
+    double inv;  // 1 / channels
 };
 
 constexpr int NORM_WAVES = 16;
 
 template <int DT, int OUT, int N> __global__ __launch_bounds__(64 * NORM_WAVES) void ogc_norm_kernel(NormArgs a) {
     constexpr int E = MxEight<DT>::E, ROWS = OUT == OGC_NORM_SAME ? 1 : 8, LANES = 64 / ROWS;  // rows of a workgroup, lanes of a row in a wavefront
-    __shared__ float part[NORM_WAVES][ROWS];
+    __shared__ double part[NORM_WAVES][ROWS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int64_t row = (int64_t)blockIdx.x * ROWS + lane / LANES;
     const int j = lane % LANES;
@@ -42,7 +43,7 @@ template <int DT, int OUT, int N> __global__ __launch_bounds__(64 * NORM_WAVES) 
     const int runs = OUT == OGC_NORM_SAME ? (limit + 512 * waves - 1) / (512 * waves) : (limit + MX_BLOCK * waves - 1) / (MX_BLOCK * waves) * 4;
 
     MxEight<DT> held[N > 0 ? N : 1];
-    float square = 0.0f;
+    double square = 0.0;  // eight squares are added up in fp32, these sums in 64 bits: the factor of a row is the rounded one, whatever its length
     const auto take = [&](MxEight<DT>& s, const MxEight<DT>& more, int c) {
         const int there = on ? a.channels - c : 0;
         float v[8];
@@ -52,8 +53,10 @@ template <int DT, int OUT, int N> __global__ __launch_bounds__(64 * NORM_WAVES) 
             s.set(v);  // (rounded: the norm is the norm of what the next layer adds to)
             if (there > 0) s.store(sum + (int64_t)c * E, there);
         }
+        float eight = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) square = __builtin_fmaf(s.get(i), s.get(i), square);
+        for (int i = 0; i < 8; ++i) eight = __builtin_fmaf(s.get(i), s.get(i), eight);
+        square += (double)eight;
     };
     if constexpr (N > 0) {
         constexpr int M = DT == OGC_F32 && N > 4 ? 4 : N;  // (registers: eight runs of fp32 have their residuals four at a time)
@@ -85,10 +88,10 @@ template <int DT, int OUT, int N> __global__ __launch_bounds__(64 * NORM_WAVES) 
     if (waves > 1) {
         if (j == 0) part[wave][lane / LANES] = square;
         __syncthreads();
-        square = 0.0f;
+        square = 0.0;
         for (int w = 0; w < waves; ++w) square += part[w][lane / LANES];
     }
-    const float f = 1.0f / __builtin_sqrtf(square * a.inv + a.eps);
+    const float f = (float)(1.0 / __builtin_sqrt(square * a.inv + (double)a.eps));
 
     const auto give = [&](const MxEight<DT>& s, int c, uint32_t& scales, int i) {
         const int there = on ? a.channels - c : 0;
@@ -200,7 +203,7 @@ ogc_status ogc_norm_run(const ogc_norm_desc* d, const void* x, const void* resid
     a.channels = d->channels;
     a.padded = mx_padded_channels(d->channels);
     a.eps = d->eps;
-    a.inv = 1.0f / (float)d->channels;
+    a.inv = 1.0 / (double)d->channels;
     const hipStream_t s = (hipStream_t)stream;
     const bool f32 = d->dtype == OGC_F32;
     if (same) f32 ? launch<OGC_F32, OGC_NORM_SAME>(a, s) : launch<OGC_BF16, OGC_NORM_SAME>(a, s);
