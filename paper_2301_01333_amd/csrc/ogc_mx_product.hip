@@ -65,59 +65,89 @@ template <int DT> MX_DEV void put4(const ProductArgs& a, int row, int n0, v4f v)
 
 constexpr int FEW_WAVES = 4;
 
-// A workgroup has 32 rows and 32 weights; its wavefronts take the channels in turn, 256 at a time, straight from memory, and add up in LDS.
-template <int DT, int XF> __global__ __launch_bounds__(64 * FEW_WAVES) void ogc_mx_few_kernel(ProductArgs a) {
+// A workgroup has NB blocks of 32 weights and 32 rows; its wavefronts take the channels in turn, 256 at a time, straight from memory into registers
+// (nothing that one of them reads is read by another of them), and add up in LDS.  Bound by memory: 32 x 32000 x 4096 with 8-bit rows 12.6 us, 5.7 TB/s; a
+// call that does not fill the chip by the latency of its loads, which are all on their way at once (32 x 8192 x 4096 4.8 us, with loads as the compiler
+// would have them 6.1).
+template <int DT, int XF, int NB> __global__ __launch_bounds__(64 * FEW_WAVES) void ogc_mx_few_kernel(ProductArgs a) {
     constexpr int PITCH = 36;  // floats of a row's 32 sums: the 16-byte pieces of eight rows are on distinct banks
     __shared__ __attribute__((aligned(16))) float sums[FEW_WAVES][32 * PITCH];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n0 = blockIdx.x, m0 = blockIdx.y;  // in blocks of 32
-    const uint8_t* w = a.w + n0 * mx_codes_of_32(OGC_MX4, a.padded) + lane * 16;
-    const uint8_t* x = a.x + m0 * mx_codes_of_32(XF, a.padded) + lane * 16;
-    const uint8_t* ws = a.ws + (int64_t)n0 * a.padded + lane * 4;
-    const uint8_t* xs = a.xs + (int64_t)m0 * a.padded + lane * 4;
-    v16f c;
+    const int n0 = blockIdx.x * NB, m0 = blockIdx.y;  // in blocks of 32
+    const int last = (a.n + 31) / 32 - 1;
+    const uint8_t *w[NB], *ws[NB];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) c[i] = 0.0f;
+    for (int i = 0; i < NB; ++i) {
+        const int b = min(n0 + i, last);
+        w[i] = a.w + b * mx_codes_of_32(OGC_MX4, a.padded) + lane * 16;
+        ws[i] = a.ws + (int64_t)b * a.padded + lane * 4;
+    }
+    const uint8_t* const x = a.x + m0 * mx_codes_of_32(XF, a.padded) + lane * 16;
+    const uint8_t* const xs = a.xs + (int64_t)m0 * a.padded + lane * 4;
+    v16f c[NB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) c[i][e] = 0.0f;
     for (int s = wave; s < a.steps; s += FEW_WAVES) {
-        Operand<OGC_MX4> p[4];
+        Operand<OGC_MX4> p[NB][4];
         Operand<XF> q[4];
+        uint32_t u[NB];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            p[i].load(w + ((int64_t)s * 4 + i) * Operand<OGC_MX4>::BYTES);
-            q[i].load(x + ((int64_t)s * 4 + i) * Operand<XF>::BYTES);
+        for (int i = 0; i < NB; ++i) u[i] = *(const uint32_t*)(ws[i] + (int64_t)s * 256);
+        const uint32_t v = *(const uint32_t*)(xs + (int64_t)s * 256);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+            for (int i = 0; i < NB; ++i) p[i][t].load(w[i] + ((int64_t)s * 4 + t) * Operand<OGC_MX4>::BYTES);
+            q[t].load(x + ((int64_t)s * 4 + t) * Operand<XF>::BYTES);
         }
-        const uint32_t u = *(const uint32_t*)(ws + (int64_t)s * 256), v = *(const uint32_t*)(xs + (int64_t)s * 256);
-        c = product<XF, 0>(p[0], q[0], c, u, v);
-        c = product<XF, 1>(p[1], q[1], c, u, v);
-        c = product<XF, 2>(p[2], q[2], c, u, v);
-        c = product<XF, 3>(p[3], q[3], c, u, v);
-    }
-    // lane l has the weights 8 q + 4 (l / 32) .. of row l % 32 in its registers 4 q ..
+        __builtin_amdgcn_sched_barrier(0);  // (all of them on their way before the first is waited for)
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-        *(v4f*)(&sums[wave][lane % 32 * PITCH + q * 8 + lane / 32 * 4]) = (v4f){c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
-    __syncthreads();
+        for (int i = 0; i < NB; ++i) {
+            c[i] = product<XF, 0>(p[i][0], q[0], c[i], u[i], v);
+            c[i] = product<XF, 1>(p[i][1], q[1], c[i], u[i], v);
+            c[i] = product<XF, 2>(p[i][2], q[2], c[i], u[i], v);
+            c[i] = product<XF, 3>(p[i][3], q[3], c[i], u[i], v);
+        }
+    }
     const int row = threadIdx.x / 8, at = threadIdx.x % 8 * 4;
-    v4f v = *(const v4f*)(&sums[0][row * PITCH + at]);
 #pragma unroll
-    for (int i = 1; i < FEW_WAVES; ++i) v += *(const v4f*)(&sums[i][row * PITCH + at]);
-    if (a.bias) {
+    for (int i = 0; i < NB; ++i) {
+        if (i > 0) __syncthreads();
+        // lane l has the weights 8 q + 4 (l / 32) .. of row l % 32 in its registers 4 q ..
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] += n0 * 32 + at + i < a.n ? a.bias[n0 * 32 + at + i] : 0.0f;
+        for (int q = 0; q < 4; ++q)
+            *(v4f*)(&sums[wave][lane % 32 * PITCH + q * 8 + lane / 32 * 4]) = (v4f){c[i][4 * q], c[i][4 * q + 1], c[i][4 * q + 2], c[i][4 * q + 3]};
+        __syncthreads();
+        const int n = (n0 + i) * 32 + at;
+        v4f v = *(const v4f*)(&sums[0][row * PITCH + at]);
+#pragma unroll
+        for (int k = 1; k < FEW_WAVES; ++k) v += *(const v4f*)(&sums[k][row * PITCH + at]);
+        if (a.bias) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] += n + k < a.n ? a.bias[n + k] : 0.0f;
+        }
+        put4<DT>(a, m0 * 32 + row, n, v);
     }
-    put4<DT>(a, m0 * 32 + row, n0 * 32 + at, v);
 }
 
 #include "ogc_mx_tile.h"
 
 namespace {
 
-// Which kernel a call takes, and how many workgroups: the same for its launch and its name.
-enum { FEW, TILE_128, TILE_256 };
+// Which kernel a call takes: the same for its launch and its name.  Few blocks of 32 x 32: wavefronts that share the channels, one block each where
+// workgroups of two would not give every compute unit two of them (m x n x k, 8-bit rows, one block / two, us: 32 x 8192 x 4096 4.8 / 5.6, 64 x 8192 x 4096
+// 6.8 / 5.9, 128 x 8192 x 4096 10.4 / 8.4).  More: tiles in LDS, from 1536 blocks on (two blocks / tiles of 128 x 128: 128 x 8192 x 4096 8.4 / 13.6, 256 x 8192 x
+// 4096 15 / 14.4).  Tiles of 256 x 256 have a compute unit to themselves, and take as long for one as for 256; two of 128 x 128 share
+// one, and a round of 512 takes 0.83 of that (4 bits, us, 128 / 256: 1024 x 4096 x 4096 13.1 / 25, 2048 x 4096 x 4096 22.0 / 26.6, 4096 x 8192 x 8192
+// 143 / 124; 8-bit rows 2048 x 4096 x 4096 30.6 / 39.9, 4096 x 8192 x 8192 216 / 189).
+enum { FEW_1, FEW_2, TILE_128, TILE_256 };
 int kernel_for(const ogc_mx_product_desc* d) {
-    const int64_t tiles = ((int64_t)d->n + 255) / 256 * (((int64_t)d->m + 255) / 256);
-    if (d->m <= 32) return FEW;
-    return tiles >= 128 ? TILE_256 : TILE_128;
+    const auto count = [&](int64_t by) { return (d->n + by - 1) / by * ((d->m + by - 1) / by); };
+    const int64_t blocks = count(32), small = count(128), large = count(256);
+    if (blocks <= 1536) return blocks < 512 ? FEW_1 : FEW_2;
+    return 0.16 + 0.67 * (double)small / 512 < (double)((large + 255) / 256) ? TILE_128 : TILE_256;
 }
 
 template <int DT, int XF, int WN, int WM, int NB, int MB> bool launch_tiles(ProductArgs a, hipStream_t s) {
@@ -136,8 +166,9 @@ template <int DT, int XF, int WN, int WM, int NB, int MB> bool launch_tiles(Prod
 template <int DT, int XF> bool launch(int which, const ProductArgs& a, hipStream_t s) {
     if (which == TILE_256) return launch_tiles<DT, XF, 2, 4, 4, 2>(a, s);
     if (which == TILE_128) return launch_tiles<DT, XF, 2, 2, 2, 2>(a, s);
-    const dim3 grid((unsigned)((a.n + 31) / 32), (unsigned)((a.m + 31) / 32));
-    hipLaunchKernelGGL((ogc_mx_few_kernel<DT, XF>), grid, dim3(64 * FEW_WAVES), 0, s, a);
+    const unsigned m = (unsigned)((a.m + 31) / 32);
+    if (which == FEW_1) hipLaunchKernelGGL((ogc_mx_few_kernel<DT, XF, 1>), dim3((a.n + 31) / 32, m), dim3(64 * FEW_WAVES), 0, s, a);
+    else hipLaunchKernelGGL((ogc_mx_few_kernel<DT, XF, 2>), dim3((a.n + 63) / 64, m), dim3(64 * FEW_WAVES), 0, s, a);
     return true;
 }
 
@@ -168,8 +199,9 @@ ogc_status ogc_mx_product_workspace_bytes(const ogc_mx_product_desc* d, size_t* 
 
 const char* ogc_mx_product_kernel_name(const ogc_mx_product_desc* d) {
     if (ogc_mx_product_validate(d) != OGC_OK) return nullptr;
-    static const char* const names[3][2][2] = {
-        {{"ogc_mx_few_kernel<0, 0>", "ogc_mx_few_kernel<0, 1>"}, {"ogc_mx_few_kernel<1, 0>", "ogc_mx_few_kernel<1, 1>"}},
+    static const char* const names[4][2][2] = {
+        {{"ogc_mx_few_kernel<0, 0, 1>", "ogc_mx_few_kernel<0, 1, 1>"}, {"ogc_mx_few_kernel<1, 0, 1>", "ogc_mx_few_kernel<1, 1, 1>"}},
+        {{"ogc_mx_few_kernel<0, 0, 2>", "ogc_mx_few_kernel<0, 1, 2>"}, {"ogc_mx_few_kernel<1, 0, 2>", "ogc_mx_few_kernel<1, 1, 2>"}},
         {{"ogc_mx_tile_kernel<0, 0, 2, 2, 2, 2>", "ogc_mx_tile_kernel<0, 1, 2, 2, 2, 2>"}, {"ogc_mx_tile_kernel<1, 0, 2, 2, 2, 2>", "ogc_mx_tile_kernel<1, 1, 2, 2, 2, 2>"}},
         {{"ogc_mx_tile_kernel<0, 0, 2, 4, 4, 2>", "ogc_mx_tile_kernel<0, 1, 2, 4, 4, 2>"}, {"ogc_mx_tile_kernel<1, 0, 2, 4, 4, 2>", "ogc_mx_tile_kernel<1, 1, 2, 4, 4, 2>"}}};
     return names[kernel_for(d)][d->dtype][d->x_format];

@@ -25,9 +25,10 @@ template <int XF, int WN, int WM, int NB, int MB> struct MxTile {
     static constexpr int LDS = S * STAGE + 2 * SCALES;
     static constexpr int PITCH = NB * 32 + 4;  // floats of a row's sums on their way out
     static_assert(WAVES * 32 * PITCH * 4 <= LDS && LDS <= 160 * 1024, "LDS");
-    static_assert(TN == WAVES && TM % WAVES == 0, "a wavefront loads whole blocks");
+    static_assert(TN % WAVES == 0 && TM % WAVES == 0, "a wavefront loads whole blocks");
+    static constexpr int OWN_N = TN / WAVES, OWN_M = TM / WAVES;
     // direct loads of a wavefront for a stage, and for the scales
-    static constexpr int LOADS = 2 + TM / WAVES * 2 * XB / 1024, SCALE_LOADS = 1 + TM / WAVES;
+    static constexpr int LOADS = OWN_N * 2 + OWN_M * 2 * XB / 1024, SCALE_LOADS = OWN_N + OWN_M;
 };
 
 // `bytes` of a wavefront's lanes: 16 or 4 each, from `from` (the same for all lanes) + 16 or 4 * lane, to LDS byte `to`
@@ -42,7 +43,7 @@ template <int N> MX_DEV void mx_meet() {  // all but the N newest loads have lan
 }
 
 template <int DT, int XF, int WN, int WM, int NB, int MB>
-__global__ __launch_bounds__(64 * WN * WM, 2) void ogc_mx_tile_kernel(ProductArgs a) {
+__global__ __launch_bounds__(64 * WN * WM, NB * MB > 8 ? 1 : 2) void ogc_mx_tile_kernel(ProductArgs a) {
     typedef MxTile<XF, WN, WM, NB, MB> T;
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     const uint32_t lds = (uint32_t)(uintptr_t)(mx_lds_u8*)smem;
@@ -56,34 +57,39 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void ogc_mx_tile_kernel(ProductArg
 
     // this wavefront's blocks to load (beyond the last one: that one again)
     const int64_t wc = mx_codes_of_32(OGC_MX4, a.padded), xc = mx_codes_of_32(XF, a.padded);
-    const int wb = min(tn * T::TN + wave, nblocks - 1);
-    const uint8_t* w = a.w + wb * wc;
-    const uint8_t* ws = a.ws + (int64_t)wb * a.padded;
-    const uint8_t* x[T::TM / T::WAVES];
-    const uint8_t* xs[T::TM / T::WAVES];
+    const uint8_t *w[T::OWN_N], *ws[T::OWN_N], *x[T::OWN_M], *xs[T::OWN_M];
 #pragma unroll
-    for (int i = 0; i < T::TM / T::WAVES; ++i) {
+    for (int i = 0; i < T::OWN_N; ++i) {
+        const int b = min(tn * T::TN + wave + i * T::WAVES, nblocks - 1);
+        w[i] = a.w + b * wc;
+        ws[i] = a.ws + (int64_t)b * a.padded;
+    }
+#pragma unroll
+    for (int i = 0; i < T::OWN_M; ++i) {
         const int b = min(tm * T::TM + wave + i * T::WAVES, mblocks - 1);
         x[i] = a.x + b * xc;
         xs[i] = a.xs + (int64_t)b * a.padded;
     }
     const uint32_t lane16 = lane * 16, lane4 = lane * 4;
     const int stages = 2 * a.steps;
-    auto issue = [&](int s, uint32_t at, auto even_c) {  // stage s into the place at byte `at`; even: and the scales of its 256 channels
-        const uint32_t to = lds + at;
-        mx_load16(to + wave * 2048, w + (int64_t)s * 2048, lane16);
-        mx_load16(to + wave * 2048 + 1024, w + (int64_t)s * 2048 + 1024, lane16);
+    // Load i of stage s into the place at byte `at`: the weights' 64 channels twice, the rows', and, of an even stage, the scales of its 256 channels.
+    auto load = [&](int s, uint32_t at, int i) {
+        const uint32_t to = lds + at, scales = lds + T::S * T::STAGE + (s / 2 & 1) * T::SCALES;
+        constexpr int PER = 2 * T::XB / 1024;  // loads of a block of rows
+        if (i < 2 * T::OWN_N) return mx_load16(to + (wave + i / 2 * T::WAVES) * 2048 + i % 2 * 1024, w[i / 2] + (int64_t)s * 2048 + i % 2 * 1024, lane16);
+        i -= 2 * T::OWN_N;
+        if (i < T::OWN_M * PER)
+            return mx_load16(to + T::W_STAGE + (wave + i / PER * T::WAVES) * 2 * T::XB + i % PER * 1024, x[i / PER] + (int64_t)s * 2 * T::XB + i % PER * 1024, lane16);
+        i -= T::OWN_M * PER;
+        if (i < T::OWN_N) return mx_load4(scales + (wave + i * T::WAVES) * 256, ws[i] + (int64_t)s * 128, lane4);
+        i -= T::OWN_N;
+        mx_load4(scales + (T::TN + wave + i * T::WAVES) * 256, xs[i] + (int64_t)s * 128, lane4);
+    };
+    auto loads_of = [](bool even) { return T::LOADS + (even ? T::SCALE_LOADS : 0); };
+    auto issue = [&](int s, uint32_t at, bool even) {
 #pragma unroll
-        for (int i = 0; i < T::TM / T::WAVES; ++i)
-#pragma unroll
-            for (int j = 0; j < 2 * T::XB / 1024; ++j)
-                mx_load16(to + T::W_STAGE + (wave + i * T::WAVES) * 2 * T::XB + j * 1024, x[i] + (int64_t)s * 2 * T::XB + j * 1024, lane16);
-        if constexpr (decltype(even_c)::value) {
-            const uint32_t scales = lds + T::S * T::STAGE + (s / 2 & 1) * T::SCALES;
-            mx_load4(scales + wave * 256, ws + (int64_t)s * 128, lane4);
-#pragma unroll
-            for (int i = 0; i < T::TM / T::WAVES; ++i) mx_load4(scales + (T::TN + wave + i * T::WAVES) * 256, xs[i] + (int64_t)s * 128, lane4);
-        }
+        for (int i = 0; i < T::LOADS + T::SCALE_LOADS; ++i)
+            if (i < loads_of(even)) load(s, at, i);
     };
     const int wn = wave % WN, wm = wave / WN;
     Operand<OGC_MX4> p[2][NB];
@@ -113,12 +119,15 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void ogc_mx_tile_kernel(ProductArg
         for (int j = 0; j < MB; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) c[i][j][e] = 0.0f;
-    auto multiply = [&](int f, auto quarter_c) {
+    auto multiply = [&](int f, auto quarter_c, auto between) {  // between: called after each instruction with its number
         constexpr int quarter = decltype(quarter_c)::value;
 #pragma unroll
         for (int j = 0; j < MB; ++j)
 #pragma unroll
-            for (int i = 0; i < NB; ++i) c[i][j] = product<XF, quarter>(p[f][i], q[f][j], c[i][j], sp[i], sq[j]);
+            for (int i = 0; i < NB; ++i) {
+                c[i][j] = product<XF, quarter>(p[f][i], q[f][j], c[i][j], sp[i], sq[j]);
+                between(j * NB + i);
+            }
     };
     uint32_t at = 0;  // the place of the stage that is worked on
     auto after = [&](uint32_t place) { return place + T::STAGE == T::S * T::STAGE ? 0 : place + T::STAGE; };
@@ -128,21 +137,28 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void ogc_mx_tile_kernel(ProductArg
         constexpr int LEFT = T::S == 4 ? 2 * T::LOADS + T::SCALE_LOADS : odd ? T::LOADS : T::LOADS + T::SCALE_LOADS;
         read(1, at, 1);
         __builtin_amdgcn_sched_barrier(0);  // (reads first: otherwise the compiler puts them behind their predecessors' use, in the same registers)
-        multiply(0, std::integral_constant<int, odd ? 2 : 0>());
+        multiply(0, std::integral_constant<int, odd ? 2 : 0>(), [](int) {});
         __builtin_amdgcn_sched_barrier(0);  // (matrix instructions are nothing that the compiler would keep on their side of assembly)
-        if constexpr (decltype(more_c)::value) {
-            mx_meet<LEFT>();
-            issue(s + T::S, at, std::integral_constant<bool, (odd ? 1 : 0) == T::S % 2>());
-        } else {
-            mx_meet<0>();
-        }
+        if constexpr (decltype(more_c)::value) mx_meet<LEFT>();
+        else mx_meet<0>();
         __builtin_amdgcn_sched_barrier(0);
+        const uint32_t freed = at;
         at = after(at);
         read(0, at, 0);  // (behind the last stage: whatever is there)
         uint32_t up[NB], uq[MB];
         if constexpr (odd) read_scales(up, uq, s / 2 + 1);
         __builtin_amdgcn_sched_barrier(0);
-        multiply(1, std::integral_constant<int, odd ? 3 : 1>());
+        // The loads of stage s + S go out between the matrix instructions: a load takes its wavefront some eighty cycles, of which an instruction covers half.
+        multiply(1, std::integral_constant<int, odd ? 3 : 1>(), [&](int k) {
+            if constexpr (decltype(more_c)::value) {
+                constexpr int COUNT = T::LOADS + ((odd ? 1 : 0) == T::S % 2 ? T::SCALE_LOADS : 0);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < COUNT; ++i)
+                    if (i * NB * MB / COUNT == k) load(s + T::S, freed, i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        });
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (odd) {
 #pragma unroll
@@ -152,11 +168,11 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void ogc_mx_tile_kernel(ProductArg
         }
     };
     // ---- the first S stages, or as many as there are (an even number)
-    issue(0, 0, std::true_type());
-    issue(1, T::STAGE, std::false_type());
+    issue(0, 0, true);
+    issue(1, T::STAGE, false);
     if (stages > 2) {
-        issue(2, 2 * T::STAGE, std::true_type());
-        if constexpr (T::S > 3) issue(3, 3 * T::STAGE, std::false_type());
+        issue(2, 2 * T::STAGE, true);
+        if constexpr (T::S > 3) issue(3, 3 * T::STAGE, false);
         asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((T::S - 1) * T::LOADS + T::SCALE_LOADS) : "memory");
     } else {
         asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(T::LOADS) : "memory");
