@@ -1,7 +1,7 @@
 """The choice of a token (include/ogc_sample.h) through the C ABI against oracle/mx.py.
 
-Tokens are equal, wherever no decision was closer than 2^-36 of the sum it is compared with: weights are off by 2^-43 of the largest each when they are rounded, the oracle's
-exponential and the kernel's by 2^-45 more, and up to 1000 of them add up here.  Log-probabilities are rounded to fp32 once: 2^-24 of their value, and 2^-30 for the sum."""
+Tokens are equal, wherever no decision was closer than vocab * 2^-42 of the sum it is compared with: weights are off by 2^-43 of the largest each when they are rounded, the
+oracle's exponential and the kernel's by 2^-45 more, and no more than all of them add up.  Log-probabilities are rounded to fp32 once: 2^-24 of their value, and 2^-30 for the sum."""
 import numpy as np
 import pytest
 
@@ -53,7 +53,7 @@ def check(logits, dtype, what, skipped=0.02, **limits):
     for r in range(rows):
         kw = {k: v[r].item() for k, v in limits.items() if v is not None}
         want, wantlog, margin = mx.sample(x[r], **kw)
-        if margin < 2.0 ** -36:
+        if margin < x.shape[1] * 2.0 ** -42:
             unsure += 1
             continue
         assert token[r] == want, (what, r, kw, int(token[r]), want, margin)
@@ -149,6 +149,35 @@ def test_strides_and_offsets(dtype):
     a, _, _ = run(x, dtype, uniform=np.full(5, 0.4), logs=False)
     b, _, _ = run(x, dtype, uniform=np.full(5, 0.4))
     assert np.array_equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sigma,temperature", [(0.02, 1.0), (1.0, 0.05), (2.0, 1.5), (40.0, 1.0), (300.0, 30.0), (1e30, 1.0), (1e-30, 1e-28)])
+def test_spreads(dtype, sigma, temperature):
+    """Flat rows, whose limits have thousands of tokens before them, and steep ones; logits and temperatures of all sizes."""
+    rng = np.random.default_rng(6)
+    x = some(rng, 4, 20011, sigma)
+    u = rng.random(4)
+    for kw in (dict(top_p=0.97), dict(top_p=0.4), dict(min_p=0.3), dict(min_p=1e-6), dict(top_p=0.9, min_p=0.01), dict(top_p=0.2, min_p=0.001), dict(top_k=300), dict(top_k=1024, top_p=0.9),
+               dict(top_k=1025, top_p=0.9, min_p=0.02), dict(top_k=19000), dict()):
+        check(x, dtype, "spread %g %g %s" % (sigma, temperature, kw), skipped=0.5, temperature=temperature, uniform=u, **kw)
+
+
+@pytest.mark.parametrize("rows,vocab", [(1, 2048), (1, 2049), (3, 8193), (64, 128000), (1, 1 << 20), (2, 300001), (300, 5000)])
+def test_parts(rows, vocab):
+    """Parts of all sizes, one and many of them, with the chosen token in each."""
+    rng = np.random.default_rng(vocab)
+    x = some(rng, rows, vocab, 2.0)
+    if rows > 8:
+        x[8:] = x[rng.integers(0, 8, rows - 8)]
+    few = np.arange(rows) if rows <= 8 else np.concatenate([np.arange(8), rng.integers(8, rows, 4)])
+    for kw in (dict(), dict(top_p=0.95), dict(min_p=0.02), dict(top_k=77)):
+        u = rng.random(rows).astype(np.float32)
+        token, logp, x64 = run(x, "f32", uniform=u, **{k: np.full(rows, v) for k, v in kw.items()})
+        for r in few:
+            want, wantlog, margin = mx.sample(x64[r], uniform=u[r].item(), **{k: np.float32(v).item() if k != "top_k" else v for k, v in kw.items()})
+            if margin >= vocab * 2.0 ** -42:
+                assert token[r] == want and abs(logp[r] - wantlog) <= 2.0 ** -24 * abs(wantlog) + 2.0 ** -30, (kw, r, token[r], want)
 
 
 def test_shares_of_many_draws():

@@ -267,6 +267,12 @@ def test_sample_pointers():
         args[at] = P + (1 if name == "logits" else 2)
         refuses(ALIGN, b.ogc_sample_run, sample(), *args)
     refuses(ALIGN, b.ogc_sample_run, sample(dtype=b.OGC_F32), P + 2, *(8 * [P]))
+    refuses(WORKSPACE, b.ogc_sample_run, sample(), *(8 * [P]), 0)
+    refuses(ALIGN, b.ogc_sample_run, sample(), *(8 * [P]), P + 8)
+    assert b.ogc_sample_workspace_bytes(sample(rows=0)) == 0
+    for rows, vocab in ((1, 1), (1, 1 << 20), (64, 128000), (65535, 100)):
+        need = b.ogc_sample_workspace_bytes(sample(rows=rows, vocab=vocab, stride=vocab))
+        assert rows * (vocab + 7) // 8 * 4 <= need <= rows * (vocab * 5 + 9000)
     b.ogc_sample_run(sample(rows=0), *(9 * [0]))
 
 
