@@ -36,14 +36,14 @@ struct SampleArgs {
     int rows, vocab;
     int parts, chunks;  // of a row: parts of `part` tokens, chunks of eight
     int part;
-    int even;           // rows are 16-byte aligned
     float* largest;     // [rows][parts]
     uint64_t* mass;     // [rows][parts]
     float* tops;        // [rows][chunks]
-    uint64_t* bins;     // [rows][parts][FINE]
+    double* bins;       // [rows][parts][FINE]
 };
 
 constexpr int THREADS = 1024, WAVES = THREADS / 64, BINS = 2048;
+static_assert(WAVES == 16, "the wavefronts' sums are a row of 16 lanes");
 constexpr int SCAN_THREADS = 256, FINE = 1024, MOST_K = 1024, MOST = 4096, MOST_PARTS = 256;  // bins of a part; tokens that are sorted
 
 // A logit as a key that compares the same way; NaN as minus infinity, -0 as 0.
@@ -60,32 +60,36 @@ template <int DT> SAMPLE_DEV float logit_at(const uint8_t* row, int i) {
     else return __builtin_bit_cast(float, (uint32_t)((const uint16_t*)row)[i] << 16);
 }
 
-// Weights of a row: multiples of 2^-42, in 64 bits.
+// Weights of a row (or of a part of it, whose largest logit is then the unit): multiples of 2^-42, in 64 bits.
 struct Weights {
     double largest, per;  // 1 / temperature
     __device__ __forceinline__ double log_of(float logit) const {
         const double x = logit;
         return x == largest ? 0.0 : (x - largest) * per;
     }
-    // 2^42 exp(x), rounded.  x / ln 2 = n + f, |f| <= 1/2; the series of exp(f ln 2) ends below 2^-47.
-    static __device__ __forceinline__ uint64_t of_log(double x) {
-        if (!(x > -29.9)) return 0;  // (below half of 2^-42)
-        const double y = x * 1.44269504088896340736;
-        const double n = __builtin_rint(y), f = (y - n) * 0.693147180559945309417;
-        double p = 1.0 / 39916800;
-        p = __builtin_fma(p, f, 1.0 / 3628800);
-        p = __builtin_fma(p, f, 1.0 / 362880);
-        p = __builtin_fma(p, f, 1.0 / 40320);
-        p = __builtin_fma(p, f, 1.0 / 5040);
-        p = __builtin_fma(p, f, 1.0 / 720);
-        p = __builtin_fma(p, f, 1.0 / 120);
-        p = __builtin_fma(p, f, 1.0 / 24);
-        p = __builtin_fma(p, f, 1.0 / 6);
-        p = __builtin_fma(p, f, 0.5);
-        p = __builtin_fma(p, f, 1.0);
-        p = __builtin_fma(p, f, 1.0);
-        const double v = __builtin_ldexp(p, (int)n + 42);  // at most 2^42
-        return __builtin_bit_cast(uint64_t, v + 0x1p52) - 0x4330000000000000ull;
+    // 2^42 2^y, rounded, for y <= 0.  y = n + f, |f| <= 1/2: added to 3 * 2^51, y leaves n in the lower word; 2^f by the polynomial of degree 9 through its
+    // values at the ten Chebyshev points, off by 2^-45.6; n goes into its exponent; and added to 2^52, what is left of the point is in the lower 52 bits.
+    static __device__ __forceinline__ uint64_t of_log2(double y) {
+        y = __builtin_fmax(y, -64.0);  // (no weight from -43 on)
+        const double t = y + 0x1.8p52, f = y - (t - 0x1.8p52);
+        double p = 0x1.b6571de2f2351p-24;
+        p = __builtin_fma(p, f, 0x1.63ef969a64d3cp-20);
+        p = __builtin_fma(p, f, 0x1.ffcb76789860fp-17);
+        p = __builtin_fma(p, f, 0x1.43088e257f341p-13);
+        p = __builtin_fma(p, f, 0x1.5d87fe908f88ap-10);
+        p = __builtin_fma(p, f, 0x1.3b2ab72b175eep-7);
+        p = __builtin_fma(p, f, 0x1.c6b08d7044119p-5);
+        p = __builtin_fma(p, f, 0x1.ebfbdff8149f2p-3);
+        p = __builtin_fma(p, f, 0x1.62e42fefa39f7p-1);
+        p = __builtin_fma(p, f, 0x1.000000000003dp+0);
+        const uint64_t bits = __builtin_bit_cast(uint64_t, p) + ((uint64_t)(((uint32_t)__builtin_bit_cast(uint64_t, t) + 42) << 20) << 32);
+        return __builtin_bit_cast(uint64_t, __builtin_bit_cast(double, bits) + 0x1p52) & 0xfffffffffffffull;
+    }
+    static __device__ __forceinline__ uint64_t of_log(double x) { return of_log2(x * 1.44269504088896340736); }
+    // of a logit, which is at most the largest: the same instructions wherever a part's weights are added up
+    __device__ __forceinline__ uint64_t of_part(float logit) const {
+        const double x = logit;
+        return of_log2(x == largest ? 0.0 : (x - largest) * (per * 1.44269504088896340736));
     }
     __device__ __forceinline__ uint64_t of(uint32_t key) const { return key == NOTHING ? 0 : of_log(log_of(logit_of(key))); }
 };
@@ -102,19 +106,28 @@ SAMPLE_DEV uint64_t shfl(uint64_t x, int from) {
     const uint32_t lo = __shfl((uint32_t)x, from), hi = __shfl((uint32_t)(x >> 32), from);
     return (uint64_t)hi << 32 | lo;
 }
-SAMPLE_DEV uint64_t shfl_up(uint64_t x, int by) {
-    const uint32_t lo = __shfl_up((uint32_t)x, by), hi = __shfl_up((uint32_t)(x >> 32), by);
+// x of another lane of the wavefront, 0 where there is none
+template <int CTRL, int ROWS> SAMPLE_DEV uint64_t moved(uint64_t x) {
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, ROWS, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), CTRL, ROWS, 0xf, false);
     return (uint64_t)hi << 32 | lo;
 }
-SAMPLE_DEV uint64_t wave_upto(uint64_t x, int lane) {  // sum over the lanes up to this one
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-        const uint64_t t = shfl_up(x, m);
-        if (lane >= m) x += t;
-    }
-    return x;
+SAMPLE_DEV uint64_t row_upto(uint64_t x) {  // sum over the lanes of 16 up to this one
+    x += moved<0x111, 0xf>(x);  // 1, 2, 4, 8 lanes before
+    x += moved<0x112, 0xf>(x);
+    x += moved<0x114, 0xf>(x);
+    return x + moved<0x118, 0xf>(x);
 }
-SAMPLE_DEV uint64_t wave_sum(uint64_t x, int lane) { return shfl(wave_upto(x, lane), 63); }
+SAMPLE_DEV uint64_t wave_upto(uint64_t x) {  // sum over the lanes up to this one
+    x = row_upto(x);
+    x += moved<0x142, 0xa>(x);  // the last lane of the 16 before, for the second and the fourth 16
+    return x + moved<0x143, 0xc>(x);  // lane 31, for the upper half
+}
+SAMPLE_DEV uint64_t lane_of(uint64_t x, int lane) {  // the same lane for all
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)x, lane), hi = __builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), lane);
+    return (uint64_t)hi << 32 | lo;
+}
+SAMPLE_DEV uint64_t wave_sum(uint64_t x) { return lane_of(wave_upto(x), 63); }
 
 // What is kept: the keys above `key`, and the first `ties` of the tokens that have it.
 struct Limit {
@@ -130,7 +143,7 @@ template <int DT> SAMPLE_DEV Limit select(WholeRow& sh, const uint8_t* row, int 
     uint32_t prefix = 0;
     uint64_t want = k, before_mass = 0;
     Limit r = outer;
-#pragma unroll
+#pragma unroll 1
     for (int digit = 0; digit < 3; ++digit) {
         const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bins = digit == 2 ? 1024 : 2048;
         __syncthreads();
@@ -161,7 +174,7 @@ template <int DT> SAMPLE_DEV Limit select(WholeRow& sh, const uint8_t* row, int 
         const bool mine = hi >= 0;
         const uint64_t m0 = mine ? sh.mass[hi] : 0, m1 = mine ? sh.mass[hi - 1] : 0;
         const uint64_t c0 = mine ? sh.count[hi] : 0, c1 = mine ? sh.count[hi - 1] : 0;
-        uint64_t ms = wave_upto(m0 + m1, lane), cs = wave_upto(c0 + c1, lane);
+        uint64_t ms = wave_upto(m0 + m1), cs = wave_upto(c0 + c1);
         if (lane == 63) sh.part[0][wave] = ms, sh.part[1][wave] = cs;
         __syncthreads();
         uint64_t all_mass = 0, all_count = 0;
@@ -213,8 +226,8 @@ template <int DT> SAMPLE_DEV void range_of(const uint8_t* row, int first, int la
             m += x >= least ? Weights::of_log(x) : 0;
         }
     }
-    mass = wave_sum(m, lane);
-    ties = (uint32_t)wave_sum(t, lane);
+    mass = wave_sum(m);
+    ties = (uint32_t)wave_sum(t);
 }
 
 // A row's limits.
@@ -243,25 +256,57 @@ SAMPLE_DEV bool by_bins(const Limits& l) { return !l.greedy && !l.top_k && (l.to
 // Where a logit is in units of 1/32 of the temperature, as a whole number; the same instructions wherever it is asked for.
 SAMPLE_DEV float place_of(float x, float fine) { return __builtin_floorf(x * fine); }
 
-// Eight neighbouring logits; NaN and what is behind the row as minus infinity.
-template <int DT> SAMPLE_DEV void eight_of(const uint8_t* row, int i, int vocab, bool even, float (&x)[8]) {
-    if (even && i + 8 <= vocab) {
-        if constexpr (DT == OGC_F32) {
-            const v4u u = *(const v4u*)(row + (int64_t)i * 4), v = *(const v4u*)(row + (int64_t)i * 4 + 16);
+// A row's chunks are the eights of its memory, not of its indices: chunk c begins with token 8 c - off, where off of the row's first bytes are missing
+// to a multiple of 16.  All chunks but the first and the last are then loaded whole, whatever the rows' stride.
+template <int DT> SAMPLE_DEV int off_of(const uint8_t* row) { return (int)((uintptr_t)row & 15) / (DT == OGC_F32 ? 4 : 2); }
+// Eight neighbouring logits from token i on (a chunk's first, perhaps before the row); what is not the row's is minus infinity.
+template <int DT> struct Eight {
+    v4u raw[DT == OGC_F32 ? 2 : 1];
+    __device__ __forceinline__ void clear() {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = __builtin_bit_cast(float, (uint32_t)u[e]), x[4 + e] = __builtin_bit_cast(float, (uint32_t)v[e]);
-        } else {
-            const v4u u = *(const v4u*)(row + (int64_t)i * 2);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = __builtin_bit_cast(float, e & 1 ? (uint32_t)u[e / 2] & 0xffff0000u : (uint32_t)u[e / 2] << 16);
+        for (int i = 0; i < (DT == OGC_F32 ? 2 : 1); ++i) {
+            const uint32_t none = DT == OGC_F32 ? 0xff800000u : 0xff80ff80u;
+            raw[i] = (v4u){none, none, none, none};
         }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = i + e < vocab ? logit_at<DT>(row, i + e) : -INFINITY;
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = x[e] == x[e] ? x[e] : -INFINITY;
-}
+    __device__ __forceinline__ void load(const uint8_t* row, int i, int vocab) {
+        if (i >= 0 && i + 8 <= vocab) whole(row, i);
+        else part(row, i, vocab);
+    }
+    __device__ __forceinline__ void whole(const uint8_t* row, int i) {
+        const uint8_t* const p = row + (int64_t)i * (DT == OGC_F32 ? 4 : 2);
+        raw[0] = *(const v4u*)p;
+        if constexpr (DT == OGC_F32) raw[1] = *(const v4u*)(p + 16);
+    }
+    __device__ __forceinline__ void part(const uint8_t* row, int i, int vocab) {
+        clear();
+#pragma unroll 1
+        for (int e = 0; e < 8; ++e) {  // (a row has two such chunks at most: short code is worth more than their time)
+            next();
+            if (i + e < 0 || i + e >= vocab) continue;
+            if constexpr (DT == OGC_F32) raw[1][3] = ((const uint32_t*)row)[i + e];
+            else raw[0][3] = (raw[0][3] & 0xffffu) | (uint32_t)((const uint16_t*)row)[i + e] << 16;
+        }
+    }
+    __device__ __forceinline__ void next() {  // logit 1 in the place of logit 0, and so on
+        if constexpr (DT == OGC_F32) {
+            const uint32_t first = raw[0][0];
+            raw[0] = (v4u){raw[0][1], raw[0][2], raw[0][3], raw[1][0]};
+            raw[1] = (v4u){raw[1][1], raw[1][2], raw[1][3], first};
+        } else {
+            const v4u t = raw[0];
+            raw[0] = (v4u){t[0] >> 16 | t[1] << 16, t[1] >> 16 | t[2] << 16, t[2] >> 16 | t[3] << 16, t[3] >> 16 | t[0] << 16};
+        }
+    }
+    __device__ __forceinline__ float get(int e) const {  // (NaN as it is)
+        if constexpr (DT == OGC_F32) return __builtin_bit_cast(float, (uint32_t)raw[e / 4][e % 4]);
+        else return __builtin_bit_cast(float, e & 1 ? (uint32_t)raw[0][e / 2] & 0xffff0000u : (uint32_t)raw[0][e / 2] << 16);
+    }
+    __device__ __forceinline__ float number(int e) const {  // NaN as minus infinity
+        const float x = get(e);
+        return x == x ? x : -INFINITY;
+    }
+};
 
 // ---- the parts of the rows.  Bound by reading them once, and by an exponential in 64 bits for each logit of the rows whose weights are all added up.
 template <int DT, int RUNS> __global__ __launch_bounds__(SCAN_THREADS) void ogc_sample_scan_kernel(SampleArgs a) {
@@ -272,19 +317,20 @@ template <int DT, int RUNS> __global__ __launch_bounds__(SCAN_THREADS) void ogc_
     const uint8_t* const row = a.logits + r * a.stride;
     const Limits l = limits_of(a, r);
     const bool fill = by_bins(l), add = !l.greedy && !l.top_k;
-    float x[RUNS][8], top = -INFINITY;
-    const int first = part * a.part + threadIdx.x * 8;
+    Eight<DT> x[RUNS];
+    float top = -INFINITY;
+    const int off = off_of<DT>(row), first = part * a.part + threadIdx.x * 8;  // (of the chunks)
 #pragma unroll
-    for (int i = 0; i < RUNS; ++i) eight_of<DT>(row, first + i * SCAN_THREADS * 8, a.vocab, a.even, x[i]);
+    for (int i = 0; i < RUNS; ++i) x[i].load(row, first + i * SCAN_THREADS * 8 - off, a.vocab);
     if (fill)
         for (int i = threadIdx.x; i < FINE; i += SCAN_THREADS) bins[i] = 0;
 #pragma unroll
     for (int i = 0; i < RUNS; ++i) {
-        float m = x[i][0];
+        float m = x[i].number(0);
 #pragma unroll
-        for (int e = 1; e < 8; ++e) m = fmaxf(m, x[i][e]);
-        const int at = first + i * SCAN_THREADS * 8;
-        if (at < a.vocab) a.tops[(int64_t)r * a.chunks + at / 8] = m;
+        for (int e = 1; e < 8; ++e) m = fmaxf(m, x[i].number(e));
+        const int at = (first + i * SCAN_THREADS * 8) / 8;
+        if (at < a.chunks) a.tops[(int64_t)r * a.chunks + at] = m;
         top = fmaxf(top, m);
     }
 #pragma unroll
@@ -304,19 +350,23 @@ template <int DT, int RUNS> __global__ __launch_bounds__(SCAN_THREADS) void ogc_
     weights.per = l.per;
     const float high = place_of(top, l.fine);
     uint64_t sum = 0;
-#pragma unroll
-    for (int i = 0; i < RUNS; ++i)
-#pragma unroll
+#pragma unroll 1
+    for (int i = 0; i < RUNS; ++i) {  // (read once more, from the caches: with all of them unrolled the code takes longer to come than the exponentials)
+        Eight<DT> y;
+        y.load(row, first + i * SCAN_THREADS * 8 - off, a.vocab);
+#pragma unroll 2
         for (int e = 0; e < 8; ++e) {
-            if (x[i][e] == -INFINITY) continue;
-            const uint64_t w = Weights::of_log(weights.log_of(x[i][e]));
+            const float v = y.number(0);
+            y.next();
+            const uint64_t w = weights.of_part(v);
             sum += w;
             if (fill && w) {
-                const float d = high - place_of(x[i][e], l.fine);
+                const float d = high - place_of(v, l.fine);
                 if (d >= 0.0f && d < (float)FINE) atomicAdd((unsigned long long*)&bins[(int)d], (unsigned long long)w);
             }
         }
-    sum = wave_sum(sum, lane);
+    }
+    sum = wave_sum(sum);
     if (lane == 0) sums[wave] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -324,15 +374,17 @@ template <int DT, int RUNS> __global__ __launch_bounds__(SCAN_THREADS) void ogc_
         a.mass[at] = sum;
     }
     if (fill)
-        for (int i = threadIdx.x; i < FINE; i += SCAN_THREADS) a.bins[at * FINE + i] = bins[i];
+        for (int i = threadIdx.x; i < FINE; i += SCAN_THREADS) a.bins[at * FINE + i] = (double)bins[i];
 }
 
 struct Chosen {
     uint64_t tokens[MOST];   // key, then the index's complement: falling, the lowest index first
-    uint32_t counts[FINE];
+    uint32_t counts[FINE], starts[FINE];
     uint64_t kept[MOST_PARTS];
+    double factor[MOST_PARTS];  // of a part's weights in the row's unit
+    int away[MOST_PARTS];       // bins between its largest logit and the row's
     uint64_t part[WAVES];
-    uint32_t count, low;
+    uint32_t count, low, crowded;
     int found;
     uint64_t before;
 };
@@ -343,26 +395,56 @@ union RowShared {
 
 // sum of x over the threads before this one; `all`: over all threads
 SAMPLE_DEV uint64_t sum_before(uint64_t x, uint64_t* part, uint64_t& all) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint64_t s = wave_upto(x, lane);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint64_t s = wave_upto(x);
     __syncthreads();
     if (lane == 63) part[wave] = s;
     __syncthreads();
-    uint64_t base = 0;
-    all = 0;
-#pragma unroll
-    for (int i = 0; i < WAVES; ++i) {
-        if (i < wave) base += part[i];
-        all += part[i];
-    }
-    return base + s - x;
+    const uint64_t w = row_upto(part[lane % WAVES]);
+    all = lane_of(w, WAVES - 1);
+    return (wave ? lane_of(w, wave - 1) : 0) + s - x;
 }
-// Sorts n tokens, falling; n a power of two from 64 on.  Neighbouring pairs up to 64 apart are one wavefront's.
-SAMPLE_DEV void sort(uint64_t* v, int n) {
-    for (int k = 2; k <= n; k *= 2)
+// Sorts n different tokens, falling.  Up to 1024, a thread each: by the upper 32 bits into 1024 bins of equal width, and within a bin by counting the larger
+// ones.  More of them, or many in a bin: by halves, where pairs up to 64 apart are one wavefront's.
+SAMPLE_DEV void sort(Chosen& sh, int n, uint32_t least, uint32_t most) {  // the least and the largest that the upper 32 bits may be
+    uint64_t* const v = sh.tokens;
+    if (n <= THREADS) {
+        const bool on = (int)threadIdx.x < n;
+        const uint64_t own = on ? v[threadIdx.x] : 0;
+        sh.counts[threadIdx.x] = 0;
+        if (threadIdx.x == 0) sh.crowded = 0;
+        __syncthreads();
+        const float scale = 1023.0f / (float)max(most - least, 1u);
+        const int bin = min((int)((float)(most - (uint32_t)(own >> 32)) * scale), FINE - 1);
+        uint32_t slot = 0;
+        if (on) slot = atomicAdd(&sh.counts[bin], 1u);
+        if (on && slot >= 48) sh.crowded = 1;
+        __syncthreads();
+        if (!sh.crowded) {
+            uint64_t all;
+            const uint32_t start = (uint32_t)sum_before(sh.counts[threadIdx.x], sh.part, all);
+            sh.starts[threadIdx.x] = start;
+            __syncthreads();
+            const uint32_t from = on ? sh.starts[bin] : 0, count = on ? sh.counts[bin] : 0;
+            if (on) v[from + slot] = own;
+            __syncthreads();
+            uint32_t larger = 0;
+            for (uint32_t j = 0; j < count; ++j) larger += v[from + j] > own;
+            __syncthreads();
+            if (on) v[from + larger] = own;
+            __syncthreads();
+            return;
+        }
+        __syncthreads();
+    }
+    int to = 64;
+    while (to < n) to *= 2;
+    for (int i = n + threadIdx.x; i < to; i += THREADS) v[i] = 0;  // zeros sort last
+    __syncthreads();
+    for (int k = 2; k <= to; k *= 2)
         for (int j = k / 2; j > 0; j /= 2) {
             if (j >= 64) __syncthreads();
-            for (int t = threadIdx.x; t < n / 2; t += THREADS) {
+            for (int t = threadIdx.x; t < to / 2; t += THREADS) {
                 const int i = 2 * t - (t & (j - 1));
                 const uint64_t x = v[i], y = v[i + j];
                 if ((x < y) == ((i & k) == 0)) v[i] = y, v[i + j] = x;
@@ -372,18 +454,17 @@ SAMPLE_DEV void sort(uint64_t* v, int n) {
         }
     __syncthreads();
 }
-SAMPLE_DEV int padded(uint64_t* v, int n) {  // zeros behind the tokens, which sort last
-    int to = 64;
-    while (to < n) to *= 2;
-    for (int i = n + threadIdx.x; i < to; i += THREADS) v[i] = 0;
-    __syncthreads();
-    return to;
-}
 SAMPLE_DEV uint32_t key_in(uint64_t token) { return (uint32_t)(token >> 32); }
 SAMPLE_DEV int index_in(uint64_t token) { return (int)~(uint32_t)token; }
 
+struct Result {  // of the thread that finds the token
+    int token = -1;
+    double log_weight = 0.0;
+    uint64_t all = 1;
+};
+
 // The row as a whole, from its logits alone.
-template <int DT> SAMPLE_DEV void whole_row(const SampleArgs& a, WholeRow& sh, const uint8_t* row, const Limits& l, const Weights& weights) {
+template <int DT> SAMPLE_DEV void whole_row(const SampleArgs& a, WholeRow& sh, const uint8_t* row, const Limits& l, const Weights& weights, Result& found) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = blockIdx.x, vocab = a.vocab;
     Limit limit = {NOTHING, 0, 0};
     if (l.top_k) limit = select<DT>(sh, row, vocab, weights, limit, false, (uint32_t)l.k, 0.0);
@@ -447,13 +528,10 @@ template <int DT> SAMPLE_DEV void whole_row(const SampleArgs& a, WholeRow& sh, c
         const uint32_t rank = ties_before + (uint32_t)__popcll(equals & ((1ull << lane) - 1));
         uint64_t w = 0;
         if (key != NOTHING && x >= least && (key > limit.key || (equal && rank < limit.ties))) w = Weights::of_log(x);
-        const uint64_t upto = before + wave_upto(w, lane);
+        const uint64_t upto = before + wave_upto(w);
         const uint64_t over = __ballot(upto > target);
         if (over) {
-            if (lane == __ffsll((unsigned long long)over) - 1) {
-                a.tokens[r] = i;
-                if (a.logs) a.logs[r] = (float)(x - log((double)total * 0x1p-42));
-            }
+            if (lane == __ffsll((unsigned long long)over) - 1) found = {i, x, total};
             return;
         }
         before = shfl(upto, 63);
@@ -461,31 +539,60 @@ template <int DT> SAMPLE_DEV void whole_row(const SampleArgs& a, WholeRow& sh, c
     }
 }
 
-// Collects the tokens of the chunks whose largest logit passes `chunk` and that pass `token` themselves; fail is set where there are more than MOST.
-template <int DT, class C, class T> SAMPLE_DEV void collect(const SampleArgs& a, Chosen& sh, const uint8_t* row, C chunk, T token) {
+// Collects the tokens whose logits are from `low` to `high`; there may be more than MOST.
+template <int DT> SAMPLE_DEV void collect(const SampleArgs& a, Chosen& sh, const uint8_t* row, float low, float high) {
+    constexpr int AHEAD = DT == OGC_F32 ? 4 : 8;  // chunks of a thread whose loads are on their way together
     const float* const tops = a.tops + (int64_t)blockIdx.x * a.chunks;
-    for (int i0 = 0; i0 < a.chunks; i0 += 4 * THREADS) {
-        float m[4];
+    const int off = off_of<DT>(row);
+    low = fmaxf(low, -3.4028234663852886e38f);  // (minus infinity is no token)
+#pragma unroll 1
+    for (int i0 = threadIdx.x; i0 < a.chunks; i0 += AHEAD * THREADS) {
+        float m[AHEAD];
+        Eight<DT> x[AHEAD];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int i = i0 + u * THREADS + threadIdx.x;
-            m[u] = i < a.chunks ? tops[i] : -INFINITY;
+        for (int u = 0; u < AHEAD; ++u) m[u] = i0 + u * THREADS < a.chunks ? tops[i0 + u * THREADS] : -INFINITY;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int i = (i0 + u * THREADS) * 8 - off;
+            if (m[u] >= low && i >= 0 && i + 8 <= a.vocab) x[u].whole(row, i);
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int i = i0 + u * THREADS + threadIdx.x;
-            if (m[u] == -INFINITY || !chunk(m[u])) continue;
-            float x[8];
-            eight_of<DT>(row, i * 8, a.vocab, a.even, x);
+        for (int u = 0; u < AHEAD; ++u) {
+            if (!(m[u] >= low)) continue;
+            const int i = (i0 + u * THREADS) * 8 - off;
+            if (i < 0 || i + 8 > a.vocab) x[u].part(row, i, a.vocab);
+            uint32_t pass = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (x[e] != -INFINITY && token(x[e])) {
-                    const uint32_t to = atomicAdd(&sh.count, 1u);
-                    if (to < MOST) sh.tokens[to] = (uint64_t)key_of(x[e]) << 32 | (uint32_t)~(uint32_t)(i * 8 + e);
-                }
+            for (int e = 0; e < 8; ++e) pass |= x[u].get(e) >= low && x[u].get(e) <= high ? 1u << e : 0u;
+            if (!pass) continue;
+            uint32_t to = atomicAdd(&sh.count, (uint32_t)__popc(pass));
+            for (; pass; pass &= pass - 1, ++to)
+                if (to < MOST) sh.tokens[to] = (uint32_t)(i + __ffs(pass) - 1);
         }
     }
     __syncthreads();
+    const int n = min((int)sh.count, MOST);
+    for (int j = threadIdx.x; j < n; j += THREADS) {  // (the logits once more: all at once, where picking them out above would be one after the other)
+        const uint32_t i = (uint32_t)sh.tokens[j];
+        sh.tokens[j] = (uint64_t)key_of(logit_at<DT>(row, (int)i)) << 32 | ~i;
+    }
+    __syncthreads();
+}
+// The key of the least logit whose place is `place` or more (a whole number, 2^23 at most from 0); -0 and 0 have keys of their own here.
+SAMPLE_DEV uint32_t first_at(float place, float fine) {
+    uint32_t low = 0x00800000u, high = 0xff7fffffu;  // keys: of the least fp32 number, of the largest
+    const float x = place / fine;
+    const uint32_t near = key_of(x);
+    if (__builtin_fabsf(x) < 0x1p120f && near > low + 16 && near < high - 16) {  // (a quotient is hardly off: most of the way at once)
+        if (place_of(logit_of(near + 8), fine) >= place) high = near + 8;
+        if (!(place_of(logit_of(near - 8), fine) >= place)) low = near - 7;
+    }
+    while (low < high) {
+        const uint32_t mid = low + (high - low) / 2;
+        if (place_of(logit_of(mid), fine) >= place) high = mid;
+        else low = mid + 1;
+    }
+    return low;
 }
 
 // The running sum that the chosen token's exceeds.
@@ -499,55 +606,39 @@ SAMPLE_DEV uint64_t goal_of(double p, uint64_t all) {
     const uint64_t goal = t < (double)all ? (uint64_t)t : all;
     return goal ? goal : 1;
 }
-SAMPLE_DEV void give(const SampleArgs& a, int r, int token, double log_weight, uint64_t all) {
-    a.tokens[r] = token;
-    if (a.logs) a.logs[r] = (float)(log_weight - log((double)all * 0x1p-42));
-}
 
-// The choice among `n` tokens, which become sorted by index.  Up to four of them a thread.
-SAMPLE_DEV void choose(const SampleArgs& a, Chosen& sh, int n, const Weights& weights, float u, int r) {
-    for (int i = threadIdx.x; i < n; i += THREADS) {  // the index's complement first: falling is the lowest index first
-        const uint64_t t = sh.tokens[i];
-        sh.tokens[i] = t << 32 | t >> 32;
-    }
+// The choice among the first n <= 1024 tokens, which become sorted by index.
+SAMPLE_DEV Result choose(Chosen& sh, int n, int vocab, const Weights& weights, float u) {
+    if ((int)threadIdx.x < n) sh.tokens[threadIdx.x] = sh.tokens[threadIdx.x] << 32 | sh.tokens[threadIdx.x] >> 32;  // the index's complement first: falling is the lowest index first
     __syncthreads();
-    sort(sh.tokens, padded(sh.tokens, n));
-    uint64_t w[4], own = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int i = threadIdx.x * 4 + e;
-        w[e] = i < n ? weights.of((uint32_t)sh.tokens[i]) : 0;
-        own += w[e];
-    }
-    uint64_t all, run = sum_before(own, sh.part, all);
-    const uint64_t target = target_of(u, all);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if (run <= target && target < run + w[e]) {
-            const uint64_t t = sh.tokens[threadIdx.x * 4 + e];
-            give(a, r, (int)~(uint32_t)(t >> 32), weights.log_of(logit_of((uint32_t)t)), all);
-        }
-        run += w[e];
-    }
+    sort(sh, n, ~(uint32_t)(vocab - 1), ~0u);
+    const uint64_t mine = (int)threadIdx.x < n ? sh.tokens[threadIdx.x] : 0;
+    const double x = (int)threadIdx.x < n ? weights.log_of(logit_of((uint32_t)mine)) : -INFINITY;
+    const uint64_t w = Weights::of_log(x);
+    uint64_t all;
+    const uint64_t run = sum_before(w, sh.part, all), target = target_of(u, all);
+    Result found;
+    if (run <= target && target < run + w) found = {(int)~(uint32_t)(mine >> 32), x, all};
+    return found;
 }
 
 // How many of the first n sorted tokens are kept by top-p and min-p; `before`: the weight ahead of them.
-SAMPLE_DEV int kept_of(Chosen& sh, int n, const Weights& weights, const Limits& l, uint64_t before, uint64_t goal) {
+template <int EACH> SAMPLE_DEV int kept_of(Chosen& sh, int n, const Weights& weights, const Limits& l, uint64_t before, uint64_t goal) {  // EACH: tokens of a thread
     if (threadIdx.x == 0) sh.found = n;
-    uint64_t w[4], own = 0;
-    double x[4];
+    uint64_t w[EACH], own = 0;
+    double x[EACH];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int i = threadIdx.x * 4 + e;
-        x[e] = i < n ? weights.log_of(logit_of(key_in(sh.tokens[i]))) : 0.0;
-        w[e] = i < n ? Weights::of_log(x[e]) : 0;
+    for (int e = 0; e < EACH; ++e) {
+        const int i = threadIdx.x * EACH + e;
+        x[e] = i < n ? weights.log_of(logit_of(key_in(sh.tokens[i]))) : -INFINITY;
+        w[e] = Weights::of_log(x[e]);
         own += w[e];
     }
     uint64_t all, run = before + sum_before(own, sh.part, all);
     int mine = n;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int i = threadIdx.x * 4 + e;
+    for (int e = 0; e < EACH; ++e) {
+        const int i = threadIdx.x * EACH + e;
         if (i < mine && (w[e] == 0 || (l.top_p && run >= goal) || !(x[e] >= l.least))) mine = i;
         run += w[e];
     }
@@ -556,114 +647,71 @@ SAMPLE_DEV int kept_of(Chosen& sh, int n, const Weights& weights, const Limits& 
     return sh.found;
 }
 
-template <int DT> __global__ __launch_bounds__(THREADS) void ogc_sample_kernel(SampleArgs a) {
-    __shared__ RowShared shared;
-    Chosen& sh = shared.chosen;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = blockIdx.x;
-    const uint8_t* const row = a.logits + r * a.stride;
+// A row's choice by top-k, and then the other limits; false: nothing was chosen.
+template <int DT> SAMPLE_DEV bool by_top_k(const SampleArgs& a, Chosen& sh, const uint8_t* row, const Limits& l, const Weights& weights, float high, float u, int r, Result& found) {
+    const float* const tops = a.tops + (int64_t)r * a.chunks;
+    const auto away = [&](float x) { return high - place_of(x, l.fine); };
+    // ---- the bin of the k-th of 1024 largest logits, a thread each
+    sh.counts[threadIdx.x] = 0;
+    if (threadIdx.x == 0) sh.count = 0, sh.low = 0xffffffffu, sh.found = FINE;
+    float m = -INFINITY;
+#pragma unroll 8
+    for (int i = threadIdx.x; i < a.chunks; i += THREADS) m = fmaxf(m, tops[i]);
+    const float d = m == -INFINITY ? (float)FINE : away(m);
+    __syncthreads();
+    if (d < (float)FINE) atomicAdd(&sh.counts[(int)d], 1u);
+    __syncthreads();
+    uint64_t all;
+    const uint64_t c = sh.counts[threadIdx.x], s = sum_before(c, sh.part, all), k = (uint64_t)l.k;
+    if (s < k && k <= s + c) sh.found = threadIdx.x;
+    __syncthreads();
+    // the smallest of those up to that bin: k tokens at least are as large.  (Fewer than k with a weight: all that have one.)
+    const bool enough = sh.found < FINE;
+    if (enough && d <= (float)sh.found) atomicMin(&sh.low, key_of(m));
+    __syncthreads();
+    const uint32_t low = enough ? sh.low : first_at(high - (float)(FINE - 1), l.fine);
+    collect<DT>(a, sh, row, logit_of(low), INFINITY);
+    int n = (int)sh.count;
+    __syncthreads();
+    if (n > MOST) return false;
+    sort(sh, n, min(low, key_of(logit_of(low))), key_of((float)weights.largest));
+    n = min(n, l.k);
+    if (l.top_p || l.min_p) {
+        sum_before((int)threadIdx.x < n ? weights.of(key_in(sh.tokens[threadIdx.x])) : 0, sh.part, all);
+        n = kept_of<1>(sh, n, weights, l, 0, goal_of(l.p, all));
+    }
+    found = choose(sh, n, a.vocab, weights, u);
+    return true;
+}
+
+// A row's choice by top-p and min-p, or without limits; false: nothing was chosen.
+template <int DT> SAMPLE_DEV bool by_parts(const SampleArgs& a, Chosen& sh, const uint8_t* row, const Limits& l, const Weights& weights, float high, float u, int r, Result& found) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool limited = l.top_p || l.min_p;
     const float* const largest = a.largest + (int64_t)r * a.parts;
     const uint64_t* const mass = a.mass + (int64_t)r * a.parts;
-    const float* const tops = a.tops + (int64_t)r * a.chunks;
-    const Limits l = limits_of(a, r);
-    const float u = a.uniform[r];
-    float top = -INFINITY;
-    for (int i = lane; i < a.parts; i += 64) top = fmaxf(top, largest[i]);
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
-    if (top == -INFINITY) {
-        if (threadIdx.x == 0) {
-            a.tokens[r] = -1;
-            if (a.logs) a.logs[r] = -INFINITY;
-        }
-        return;
-    }
-    if (l.greedy) {
-        if (threadIdx.x == 0) sh.found = 0x7fffffff;
-        __syncthreads();
-        for (int i = threadIdx.x; i < a.chunks; i += THREADS)
-            if (tops[i] == top) {
-                atomicMin(&sh.found, i);
-                break;
-            }
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            float x[8];
-            eight_of<DT>(row, sh.found * 8, a.vocab, a.even, x);
-            int e = 0;
-            while (x[e] != top && e < 7) ++e;
-            a.tokens[r] = sh.found * 8 + e;
-            if (a.logs) a.logs[r] = 0.0f;
-        }
-        return;
-    }
-    Weights weights;
-    weights.largest = top;
-    weights.per = l.per;
-    const float high = place_of(top, l.fine);
+    const double* const bins = a.bins + (int64_t)r * a.parts * FINE;
     const auto away = [&](float x) { return high - place_of(x, l.fine); };
-    const bool limited = l.top_k || l.top_p || l.min_p;
-    // places are whole numbers, and near enough to where the logits are, up to 2^22
-    if (limited && (!(__builtin_fabsf(high) < 0x1p22f) || (l.top_k && l.k > MOST_K))) return whole_row<DT>(a, shared.whole, row, l, weights);
-
-    if (l.top_k) {
-        // ---- the bin of the k-th of the largest-of-eight
-        sh.counts[threadIdx.x] = 0;
-        if (threadIdx.x == 0) sh.count = 0, sh.low = 0xffffffffu, sh.found = FINE;
-        __syncthreads();
-        for (int i = threadIdx.x; i < a.chunks; i += THREADS) {
-            const float d = away(tops[i]);
-            if (d < (float)FINE) atomicAdd(&sh.counts[(int)d], 1u);
-        }
-        __syncthreads();
-        uint64_t all;
-        const uint64_t c = sh.counts[threadIdx.x], s = sum_before(c, sh.part, all), k = (uint64_t)l.k;
-        if (s < k && k <= s + c) sh.found = threadIdx.x;
-        __syncthreads();
-        const float bin = (float)sh.found;
-        // the smallest of those up to that bin: k tokens at least are as large.  (Fewer than k with a weight: all of them.)
-        if (sh.found < FINE) {
-            uint32_t low = 0xffffffffu;
-            for (int i = threadIdx.x; i < a.chunks; i += THREADS)
-                if (away(tops[i]) <= bin) low = min(low, key_of(tops[i]));
-            if (low != 0xffffffffu) atomicMin(&sh.low, low);
-            __syncthreads();
-            const float least = logit_of(sh.low);
-            collect<DT>(a, sh, row, [&](float m) { return m >= least; }, [&](float x) { return x >= least; });
-        } else {
-            collect<DT>(a, sh, row, [&](float m) { return away(m) < (float)FINE; }, [&](float x) { return away(x) < (float)FINE; });
-        }
-        int n = (int)sh.count;
-        __syncthreads();
-        if (n > MOST) return whole_row<DT>(a, shared.whole, row, l, weights);
-        sort(sh.tokens, padded(sh.tokens, n));
-        n = min(n, l.k);
-        if (l.top_p || l.min_p) {
-            uint64_t own = 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) own += threadIdx.x * 4 + e < n ? weights.of(key_in(sh.tokens[threadIdx.x * 4 + e])) : 0;
-            sum_before(own, sh.part, all);
-            n = kept_of(sh, n, weights, l, 0, goal_of(l.p, all));
-        }
-        return choose(a, sh, n, weights, u, r);
+    if ((int)threadIdx.x < a.parts) {
+        const float m = largest[threadIdx.x];
+        const double f = m == (float)weights.largest ? 1.0 : exp(((double)m - weights.largest) * l.per);
+        const float d = away(m);
+        sh.factor[threadIdx.x] = f > 0.0 ? f : 0.0;
+        sh.away[threadIdx.x] = m > -INFINITY && d < (float)FINE ? (int)d : FINE;
     }
-
-    // ---- without top-k: the parts' weights in the row's unit
-    const auto factor = [&](int p) {
-        const double f = largest[p] == top ? 1.0 : exp(((double)largest[p] - (double)top) * l.per);
-        return f > 0.0 ? f : 0.0;
-    };
-    const auto in_row = [&](uint64_t mass, int p) { return (uint64_t)((double)mass * factor(p)); };
+    if (threadIdx.x == 0) sh.count = 0, sh.found = FINE - 1;
+    __syncthreads();
+    const auto in_row = [&](uint64_t mass, int p) { return (uint64_t)((double)mass * sh.factor[p]); };
     int from = FINE, kept = 0;  // kept: all of the bins before `from`, and the first `kept` sorted tokens
     if (limited) {
         // ---- bins of the row, a thread each
-        uint64_t b = 0;
+        double of_bin = 0.0;  // (the parts always one after the other)
+#pragma unroll 8
         for (int p = 0; p < a.parts; ++p) {
-            const float off = high - place_of(largest[p], l.fine);
-            if (largest[p] == -INFINITY || !(off < (float)FINE)) continue;
-            const int i = (int)threadIdx.x - (int)off;
-            if (i >= 0) b += in_row(a.bins[((int64_t)r * a.parts + p) * FINE + i], p);
+            const int i = (int)threadIdx.x - sh.away[p];  // (a part of no use is a whole row of bins away)
+            of_bin += i >= 0 ? bins[(int64_t)p * FINE + i] * sh.factor[p] : 0.0;
         }
-        if (threadIdx.x == 0) sh.count = 0, sh.found = FINE - 1;
+        const uint64_t b = (uint64_t)of_bin;
         uint64_t all;
         const uint64_t s = sum_before(b, sh.part, all), goal = goal_of(l.p, all);
         if (l.top_p && s < goal && goal <= s + b) sh.found = threadIdx.x;
@@ -681,71 +729,137 @@ template <int DT> __global__ __launch_bounds__(THREADS) void ogc_sample_kernel(S
         if ((int)threadIdx.x == from) sh.before = s;
         __syncthreads();
         const uint64_t before = sh.before;
-        const float f = (float)from, t = (float)to;
-        collect<DT>(a, sh, row, [&](float m) { return away(m) <= t; }, [&](float x) { const float d = away(x); return d >= f && d <= t; });
+        // (up to the last logit that is not in the bins before)
+        const uint32_t low = first_at(high - (float)to, l.fine), behind = from ? first_at(high - (float)(from - 1), l.fine) - 1 : key_of((float)weights.largest);
+        collect<DT>(a, sh, row, logit_of(low), from ? logit_of(behind) : INFINITY);
         const int n = (int)sh.count;
         __syncthreads();
-        if (n > MOST) return whole_row<DT>(a, shared.whole, row, l, weights);
-        sort(sh.tokens, padded(sh.tokens, n));
-        kept = kept_of(sh, n, weights, l, before, goal);
+        if (n > MOST) return false;
+        sort(sh, n, min(low, key_of(logit_of(low))), max(behind, key_of(logit_of(behind))));
+        kept = n <= THREADS ? kept_of<1>(sh, n, weights, l, before, goal) : kept_of<MOST / THREADS>(sh, n, weights, l, before, goal);
     }
     // ---- the part that has the token: what is kept of each
+    const int off = off_of<DT>(row);
     const uint64_t end = kept ? sh.tokens[kept - 1] : ~0ull;  // the last of the sorted tokens that are kept
-    if (threadIdx.x < MOST_PARTS) sh.kept[threadIdx.x] = 0;
+    if ((int)threadIdx.x < a.parts) sh.kept[threadIdx.x] = limited ? 0 : in_row(mass[threadIdx.x], threadIdx.x);
     __syncthreads();
     for (int i = threadIdx.x; i < kept; i += THREADS)
-        atomicAdd((unsigned long long*)&sh.kept[index_in(sh.tokens[i]) / a.part], (unsigned long long)weights.of(key_in(sh.tokens[i])));
-    if (limited) {
+        atomicAdd((unsigned long long*)&sh.kept[(index_in(sh.tokens[i]) + off) / a.part], (unsigned long long)weights.of(key_in(sh.tokens[i])));
+    if (limited)
         for (int p = wave; p < a.parts; p += WAVES) {
-            const float off = high - place_of(largest[p], l.fine);
-            if (largest[p] == -INFINITY || !(off < (float)from)) continue;
-            uint64_t m = 0;
-            for (int i = lane; i < from - (int)off; i += 64) m += a.bins[((int64_t)r * a.parts + p) * FINE + i];
-            m = wave_sum(m, lane);
-            if (lane == 0) atomicAdd((unsigned long long*)&sh.kept[p], (unsigned long long)in_row(m, p));
+            const int count = from - sh.away[p];
+            if (count <= 0) continue;
+            double m = 0.0;
+#pragma unroll 8
+            for (int i = lane; i < count; i += 64) m += bins[(int64_t)p * FINE + i];
+            const uint64_t here = wave_sum((uint64_t)m);
+            if (lane == 0) atomicAdd((unsigned long long*)&sh.kept[p], (unsigned long long)in_row(here, p));
         }
-    } else if (threadIdx.x < a.parts) {
-        sh.kept[threadIdx.x] = in_row(mass[threadIdx.x], threadIdx.x);
-    }
-    if (threadIdx.x == 0) sh.found = 0;
     __syncthreads();
-    const uint64_t own = threadIdx.x < a.parts ? sh.kept[threadIdx.x] : 0;
+    const uint64_t own = (int)threadIdx.x < a.parts ? sh.kept[threadIdx.x] : 0;
     uint64_t total, run = sum_before(own, sh.part, total);
     const uint64_t target = target_of(u, total);
     if (run <= target && target < run + own) sh.found = threadIdx.x, sh.before = run;
     __syncthreads();
     // ---- its tokens, in the part's own unit
     const int p = sh.found;
-    const double f = factor(p), rest = (double)(target - sh.before) / f;
+    const double rest = (double)(target - sh.before) / sh.factor[p];
     Weights near = weights;
     near.largest = largest[p];
-    const int at = p * a.part + (int)threadIdx.x * 8;
-    uint64_t w[8], mine = 0;
-    float x[8];
-    const bool here = (int)threadIdx.x * 8 < a.part && at < a.vocab;
-    if (here) eight_of<DT>(row, at, a.vocab, a.even, x);
-#pragma unroll
+    const int at = p * a.part + (int)threadIdx.x * 8 - off;
+    Eight<DT> x;
+    if ((int)threadIdx.x * 8 < a.part) x.load(row, at, a.vocab);
+    else x.clear();
+    const auto weight = [&](float v, int e) -> uint64_t {
+        const uint64_t token = (uint64_t)key_of(v) << 32 | (uint32_t)~(uint32_t)(at + e);
+        return v > -INFINITY && (!limited || away(v) < (float)from || token >= end) ? near.of_part(v) : 0;
+    };
+    uint64_t mine = 0, all;
+#pragma unroll 1
     for (int e = 0; e < 8; ++e) {
-        w[e] = 0;
-        if (!here || x[e] == -INFINITY) continue;
-        const uint64_t token = (uint64_t)key_of(x[e]) << 32 | (uint32_t)~(uint32_t)(at + e);
-        if (!limited || away(x[e]) < (float)from || token >= end) w[e] = Weights::of_log(near.log_of(x[e]));
-        mine += w[e];
+        mine += weight(x.number(0), e);
+        x.next();
     }
-    uint64_t all;
     run = sum_before(mine, sh.part, all);
     const uint64_t goal = rest < (double)all && (uint64_t)rest < all ? (uint64_t)rest : all - 1;
+    if (run <= goal && goal < run + mine) {
+#pragma unroll 1
+        for (int e = 0; e < 8; ++e) {
+            const uint64_t w = weight(x.number(0), e);
+            if (goal < run + w) {
+                found = {at + e, weights.log_of(x.number(0)), total};
+                break;
+            }
+            run += w;
+            x.next();
+        }
+    }
+    return true;
+}
+
+template <int DT> __global__ __launch_bounds__(THREADS) void ogc_sample_kernel(SampleArgs a) {
+    __shared__ RowShared shared;
+    Chosen& sh = shared.chosen;
+    const int lane = threadIdx.x & 63, r = blockIdx.x;
+    const uint8_t* const row = a.logits + r * a.stride;
+    const Limits l = limits_of(a, r);
+    const float u = a.uniform[r];
+    float top = -INFINITY;
+    for (int i = lane; i < a.parts; i += 64) top = fmaxf(top, a.largest[(int64_t)r * a.parts + i]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        if (run <= goal && goal < run + w[e]) give(a, r, at + e, weights.log_of(x[e]), total);
-        run += w[e];
+    for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
+    if (top == -INFINITY) {
+        if (threadIdx.x == 0) {
+            a.tokens[r] = -1;
+            if (a.logs) a.logs[r] = -INFINITY;
+        }
+        return;
+    }
+    if (l.greedy) {
+        const float* const tops = a.tops + (int64_t)r * a.chunks;
+        if (threadIdx.x == 0) sh.found = 0x7fffffff;
+        __syncthreads();
+        for (int i = threadIdx.x; i < a.chunks; i += THREADS)
+            if (tops[i] == top) {
+                atomicMin(&sh.found, i);
+                break;
+            }
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            const int at = sh.found * 8 - off_of<DT>(row);
+            Eight<DT> x;
+            x.load(row, at, a.vocab);
+            int first = 7;
+#pragma unroll
+            for (int e = 6; e >= 0; --e)
+                if (x.get(e) == top) first = e;
+            a.tokens[r] = at + first;
+            if (a.logs) a.logs[r] = 0.0f;
+        }
+        return;
+    }
+    Weights weights;
+    weights.largest = top;
+    weights.per = l.per;
+    const float high = place_of(top, l.fine);
+    // places are whole numbers, and near enough to where the logits are, up to 2^22
+    bool done = !(l.top_k || l.top_p || l.min_p) || (__builtin_fabsf(high) < 0x1p22f && (!l.top_k || l.k <= MOST_K));
+    Result found;
+    if (done) done = l.top_k ? by_top_k<DT>(a, sh, row, l, weights, high, u, r, found) : by_parts<DT>(a, sh, row, l, weights, high, u, r, found);
+    if (!done) whole_row<DT>(a, shared.whole, row, l, weights, found);
+    if (found.token >= 0) {
+        a.tokens[r] = found.token;
+        if (a.logs) a.logs[r] = (float)(found.log_weight - log((double)found.all * 0x1p-42));
     }
 }
 
+// Chunks and parts of a row that begins up to seven tokens behind a multiple of 16 bytes.
+int chunks_of(const ogc_sample_desc* d) { return (d->vocab + 7 + 7) / 8; }
+int parts_of(const ogc_sample_desc* d, int part) { return (d->vocab + 7 + part - 1) / part; }
 // Tokens of a part: as many as leave the chip enough workgroups, 8192 at most; 256 parts of a row at most.
 int part_of(const ogc_sample_desc* d) {
     int part = 8192;
-    while (part > 2048 && (int64_t)d->rows * ((d->vocab + part - 1) / part) < 512 && (d->vocab + part / 2 - 1) / (part / 2) <= MOST_PARTS) part /= 2;
+    while (part > 2048 && (int64_t)d->rows * parts_of(d, part) < 512 && parts_of(d, part / 2) <= MOST_PARTS) part /= 2;
     return part;
 }
 
@@ -773,7 +887,7 @@ ogc_status ogc_sample_workspace_bytes(const ogc_sample_desc* d, size_t* bytes) {
     const ogc_status st = ogc_sample_validate(d);
     if (st != OGC_OK) return st;
     if (!bytes) return OGC_ERR_INVALID_ARG;
-    const size_t part = (size_t)part_of(d), parts = (d->vocab + part - 1) / part, chunks = (d->vocab + 7) / 8;
+    const size_t part = (size_t)part_of(d), parts = parts_of(d, (int)part), chunks = chunks_of(d);
     *bytes = d->rows * (parts * (FINE * sizeof(uint64_t) + sizeof(uint64_t) + sizeof(float)) + chunks * sizeof(float));
     return OGC_OK;
 }
@@ -803,11 +917,10 @@ ogc_status ogc_sample_run(const ogc_sample_desc* d, const void* logits, const fl
     a.rows = d->rows;
     a.vocab = d->vocab;
     a.part = part_of(d);
-    a.parts = (d->vocab + a.part - 1) / a.part;
-    a.chunks = (d->vocab + 7) / 8;
-    a.even = ((uintptr_t)logits | (uintptr_t)a.stride) % 16 == 0;
-    a.bins = (uint64_t*)workspace;
-    a.mass = a.bins + (size_t)d->rows * a.parts * FINE;
+    a.parts = parts_of(d, a.part);
+    a.chunks = chunks_of(d);
+    a.bins = (double*)workspace;
+    a.mass = (uint64_t*)a.bins + (size_t)d->rows * a.parts * FINE;
     a.largest = (float*)(a.mass + (size_t)d->rows * a.parts);
     a.tops = a.largest + (size_t)d->rows * a.parts;
     const hipStream_t s = (hipStream_t)stream;

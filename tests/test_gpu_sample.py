@@ -163,6 +163,18 @@ def test_spreads(dtype, sigma, temperature):
         check(x, dtype, "spread %g %g %s" % (sigma, temperature, kw), skipped=0.5, temperature=temperature, uniform=u, **kw)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_limits_next_to_zero(dtype):
+    """The bins' limits at logits of 0, -0 and the smallest numbers, where many tokens are."""
+    rng = np.random.default_rng(8)
+    x = rng.choice([0.0, -0.0, 1e-40, -1e-40, 1e-3, -1e-3, 0.5, -0.5, -0.03125, 0.03125], size=(6, 3000))
+    x[:, 7] = [0.0, 0.25, 1.0, 0.03125, 2.0, 0.5]
+    u = rng.random(6)
+    for kw in (dict(top_p=0.5), dict(top_p=0.9), dict(min_p=0.96), dict(min_p=0.5), dict(top_p=0.7, min_p=0.9), dict(top_k=700), dict()):
+        check(x, dtype, "zeros %s" % kw, skipped=0.5, uniform=u, **kw)
+        check(x, dtype, "zeros %s" % kw, skipped=0.5, uniform=u, temperature=0.031, **kw)
+
+
 @pytest.mark.parametrize("rows,vocab", [(1, 2048), (1, 2049), (3, 8193), (64, 128000), (1, 1 << 20), (2, 300001), (300, 5000)])
 def test_parts(rows, vocab):
     """Parts of all sizes, one and many of them, with the chosen token in each."""
