@@ -354,10 +354,9 @@ template <int DT, int RUNS> __global__ __launch_bounds__(SCAN_THREADS) void ogc_
     for (int i = 0; i < RUNS; ++i) {  // (read once more, from the caches: with all of them unrolled the code takes longer to come than the exponentials)
         Eight<DT> y;
         y.load(row, first + i * SCAN_THREADS * 8 - off, a.vocab);
-#pragma unroll 2
+#pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float v = y.number(0);
-            y.next();
+            const float v = y.number(e);
             const uint64_t w = weights.of_part(v);
             sum += w;
             if (fill && w) {
@@ -550,7 +549,9 @@ template <int DT> SAMPLE_DEV void collect(const SampleArgs& a, Chosen& sh, const
         float m[AHEAD];
         Eight<DT> x[AHEAD];
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) m[u] = i0 + u * THREADS < a.chunks ? tops[i0 + u * THREADS] : -INFINITY;
+        for (int u = 0; u < AHEAD; ++u) m[u] = tops[min(i0 + u * THREADS, a.chunks - 1)];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) m[u] = i0 + u * THREADS < a.chunks ? m[u] : -INFINITY;
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int i = (i0 + u * THREADS) * 8 - off;
@@ -655,8 +656,14 @@ template <int DT> SAMPLE_DEV bool by_top_k(const SampleArgs& a, Chosen& sh, cons
     sh.counts[threadIdx.x] = 0;
     if (threadIdx.x == 0) sh.count = 0, sh.low = 0xffffffffu, sh.found = FINE;
     float m = -INFINITY;
-#pragma unroll 8
-    for (int i = threadIdx.x; i < a.chunks; i += THREADS) m = fmaxf(m, tops[i]);
+#pragma unroll 1
+    for (int i = threadIdx.x; i < a.chunks; i += 8 * THREADS) {
+        float t[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) t[u] = tops[min(i + u * THREADS, a.chunks - 1)];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) m = i + u * THREADS < a.chunks ? fmaxf(m, t[u]) : m;
+    }
     const float d = m == -INFINITY ? (float)FINE : away(m);
     __syncthreads();
     if (d < (float)FINE) atomicAdd(&sh.counts[(int)d], 1u);
@@ -706,10 +713,17 @@ template <int DT> SAMPLE_DEV bool by_parts(const SampleArgs& a, Chosen& sh, cons
     if (limited) {
         // ---- bins of the row, a thread each
         double of_bin = 0.0;  // (the parts always one after the other)
-#pragma unroll 8
-        for (int p = 0; p < a.parts; ++p) {
-            const int i = (int)threadIdx.x - sh.away[p];  // (a part of no use is a whole row of bins away)
-            of_bin += i >= 0 ? bins[(int64_t)p * FINE + i] * sh.factor[p] : 0.0;
+#pragma unroll 1
+        for (int p0 = 0; p0 < a.parts; p0 += 8) {
+            double b[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {  // (a part of no use is a whole row of bins away)
+                const int p = min(p0 + u, a.parts - 1);
+                b[u] = bins[(int64_t)p * FINE + max((int)threadIdx.x - sh.away[p], 0)];
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (p0 + u < a.parts && (int)threadIdx.x >= sh.away[p0 + u]) of_bin += b[u] * sh.factor[p0 + u];
         }
         const uint64_t b = (uint64_t)of_bin;
         uint64_t all;
