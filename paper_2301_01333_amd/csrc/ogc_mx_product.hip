@@ -139,15 +139,22 @@ namespace {
 // Which kernel a call takes: the same for its launch and its name.  Few blocks of 32 x 32: wavefronts that share the channels, one block each where
 // workgroups of two would not give every compute unit two of them (m x n x k, 8-bit rows, one block / two, us: 32 x 8192 x 4096 4.8 / 5.6, 64 x 8192 x 4096
 // 6.8 / 5.9, 128 x 8192 x 4096 10.4 / 8.4).  More: tiles in LDS, from 1536 blocks on (two blocks / tiles of 128 x 128: 128 x 8192 x 4096 8.4 / 13.6, 256 x 8192 x
-// 4096 15 / 14.4).  Tiles of 256 x 256 have a compute unit to themselves, and take as long for one as for 256; two of 128 x 128 share
-// one, and a round of 512 takes 0.83 of that (4 bits, us, 128 / 256: 1024 x 4096 x 4096 13.1 / 25, 2048 x 4096 x 4096 22.0 / 26.6, 4096 x 8192 x 8192
-// 143 / 124; 8-bit rows 2048 x 4096 x 4096 30.6 / 39.9, 4096 x 8192 x 8192 216 / 189).
+// 4096 15 / 14.4, 4096 x 4096 x 512 18.8 / 12.8).
+// Tiles of 256 x 256 have a compute unit to themselves, so that 256 of them take as long as one, and no product hides their first loads and last stores;
+// two of 128 x 128 share a compute unit, but pull twice the bytes through LDS.  A round of 512 small tiles takes 3 + 0.51 us for 128 channels (half of them 0.6
+// of that), one of 256 large ones 7 + 0.83, with 8-bit rows 3 + 0.79 and 7 + 1.36, fitted to small / large, us: 4 bits 4096 x 4096 x 512 12.8 / 12.9, 8192 x 8192 x 512
+// 37.8 / 41.6, 8192 x 8192 x 1024 55 / 59, 4096 x 4096 x 2048 24.7 / 23.2, 2048 x 2048 x 8192 21.6 / 42.3, 8192 x 8192 x 8192 285 / 242; 8-bit rows 4096 x 4096 x 512
+// 15.0 / 15.4, 4096 x 4096 x 1024 21.4 / 20.5, 4096 x 8192 x 8192 216 / 189.
 enum { FEW_1, FEW_2, TILE_128, TILE_256 };
 int kernel_for(const ogc_mx_product_desc* d) {
     const auto count = [&](int64_t by) { return (d->n + by - 1) / by * ((d->m + by - 1) / by); };
     const int64_t blocks = count(32), small = count(128), large = count(256);
     if (blocks <= 1536) return blocks < 512 ? FEW_1 : FEW_2;
-    return 0.16 + 0.67 * (double)small / 512 < (double)((large + 255) / 256) ? TILE_128 : TILE_256;
+    const double stages = mx_padded_channels(d->k) / 128, rest = small % 512 == 0 ? 0.0 : small % 512 <= 256 ? 0.6 : 1.0;
+    const bool eight = d->x_format == OGC_MX8;
+    const double of_small = ((double)(small / 512) + rest) * (3.0 + (eight ? 0.79 : 0.51) * stages);
+    const double of_large = (double)((large + 255) / 256) * (7.0 + (eight ? 1.36 : 0.83) * stages);
+    return of_small < of_large ? TILE_128 : TILE_256;
 }
 
 template <int DT, int XF, int WN, int WM, int NB, int MB> bool launch_tiles(ProductArgs a, hipStream_t s) {

@@ -1,0 +1,159 @@
+"""A decoder's layer from norm to feed-forward and the choice of a token (paper_2301_01333_amd/decoder_layer.py): what it refuses, and a run of its operators one after
+the other as a program uses them, against float64."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import mx
+from paper_2301_01333_amd import decoder_layer as dl
+from paper_2301_01333_amd.decoder import DecoderAttention
+
+
+@pytest.mark.parametrize("x", [
+    torch.zeros(8), torch.zeros(2, 3, 8), torch.zeros(4, 16, dtype=torch.float16), torch.zeros(16, 4).t(), torch.zeros(4, 16)[:, ::2], torch.zeros(4, 15)[:, :14], torch.zeros(4, 16),
+    torch.zeros(1, 16).expand(4, 16)])
+def test_rows_that_are_refused(x):  # (the last but one, of the right form, because it is not on a GPU)
+    with pytest.raises(ValueError):
+        dl.check_matrix(x, "rows")
+    with pytest.raises(ValueError):
+        dl.MxMatrix.write(x, "mx8")
+    with pytest.raises(ValueError):
+        dl.add_norm(x, None, torch.ones(16))
+
+
+def test_formats_and_limits_that_are_refused():
+    with pytest.raises(ValueError):
+        dl.MxMatrix("mx6", 4, 32)
+    for kw in (dict(temperature=torch.ones(3)), dict(top_k=torch.ones(2)), dict(top_p=torch.ones(2, dtype=torch.float64)), dict(min_p=torch.ones(2))):
+        with pytest.raises(ValueError):
+            dl.TokenChoice(2, 10, torch.float32, **kw)
+    with pytest.raises(ValueError):
+        dl.TokenChoice(2, 10, torch.float16)
+
+
+def layer(dtype, rows, seed=0, c=256, hidden=320, hq=4, hk=2, d=32, batch=2, tokens=64):
+    g = torch.Generator().manual_seed(seed)
+    w = lambda n, k: (torch.randn((n, k), generator=g) * k ** -0.5).cuda()  # noqa: E731
+    norms = [(1 + 0.1 * torch.randn(c, generator=g)).cuda() for _ in range(2)]
+    return dl.DecoderLayer(DecoderAttention(dtype, hq, hk, d, batch, tokens), w((hq + 2 * hk) * d, c), w(c, hq * d), w(2 * hidden, c), w(c, hidden), *norms, rows=rows)
+
+
+def f64(x):
+    return (x.read(torch.float32) if isinstance(x, dl.MxMatrix) else x).double().cpu().numpy()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", ["mx8", "mx4"])
+def test_a_layer_is_its_operators_one_after_the_other(dtype, rows):
+    """Every operator's result from what the one before left, in float64; the layer's result is theirs, bit for bit."""
+    t = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    half = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}[dtype]
+    a, b = layer(dtype, rows), layer(dtype, rows)
+    lengths = [9, 14]
+    g = torch.Generator().manual_seed(7)
+    x, more = (torch.randn((23, 256), generator=g).to(t).cuda() for _ in range(2))
+    for step in range(3):  # the prompts, then two tokens
+        got = a.prefill(x, more, lengths) if step == 0 else a.step(x[:2], more[:2])
+        if step:
+            x, more = x[:2], more[:2]
+        s, n1 = dl.add_norm(x, more, b.norm_attention, b.eps, rows)
+        s64 = (x.float() + more.float()).to(t).double().cpu().numpy()
+        assert np.array_equal(f64(s), s64)
+        # a normed row in its format: within half a step of the value, 2^-4 (MX8) or 1/4 and a quarter of the largest scale (MX4: 1/4 of a sixth of the group's largest and up)
+        want, top = mx.norm(s64, f64(b.norm_attention), b.eps), np.abs(mx.norm(s64, f64(b.norm_attention), b.eps)).max()
+        assert (np.abs(f64(n1) - want) <= (np.abs(want) * 0.0626 + top * 2.0 ** -16 if rows == "mx8" else np.abs(want) * 0.251 + top / 10)).all()
+        qkv = b.qkv(n1, t)
+        exact = f64(n1) @ f64(b.qkv.weight).T
+        slack = 1e-3 * np.abs(f64(n1)).max() * np.abs(f64(b.qkv.weight)).max()  # 64 * 2^-13 of the largest products of each of four instructions at most is 3e-2 of it; measured far less
+        assert (np.abs(f64(qkv) - exact) <= half * np.abs(exact) + 32 * slack).all()
+        heads = qkv.unflatten(1, (-1, 32))
+        o = b.attention.prefill(heads, lengths) if step == 0 else b.attention.step(heads)
+        update = b.out(dl.MxMatrix.write(o.flatten(1), rows), t)
+        s2, n2 = dl.add_norm(update, s, b.norm_feed_forward, b.eps, rows)
+        gu = b.gate_up(n2, t)
+        gated = dl.MxMatrix.write(gu, rows, gate=True)
+        want = mx.gated(f64(gu)[:, :320], f64(gu)[:, 320:])
+        top = np.abs(want).max()
+        assert (np.abs(f64(gated) - want) <= (np.abs(want) * 0.0626 + top * 2.0 ** -16 if rows == "mx8" else np.abs(want) * 0.251 + top / 10)).all()
+        update2 = b.down(gated, t)
+        assert torch.equal(got[0], s2) and torch.equal(got[1], update2)
+        assert torch.isfinite(got[1]).all()
+
+
+@pytest.mark.gpu
+def test_a_layer_is_near_the_one_without_formats():
+    """Against the same weights in float64 without quantized rows: four times in a row each value moves by 2^-4 of itself at most."""
+    a = layer("f32", "mx8", seed=3)
+    x = torch.randn((23, 256), generator=torch.Generator().manual_seed(1)).cuda()
+    stream, update = a.prefill(x, None, [9, 14])
+    assert torch.equal(stream[:0], x[:0])
+    x64, w = f64(x), [f64(p.weight) for p in (a.qkv, a.out, a.gate_up, a.down)]
+    qkv = (mx.norm(x64, f64(a.norm_attention), a.eps) @ w[0].T).reshape(23, 8, 32)
+    at, o = 0, []
+    for n in (9, 14):
+        q, k, v = qkv[at:at + n, :4], qkv[at:at + n, 4:6], qkv[at:at + n, 6:]
+        pos = np.arange(n)[:, None] * 10000.0 ** (-np.arange(0, 32, 2) / 32)
+        turn = lambda z: np.concatenate([z[..., :16] * np.cos(pos)[:, None] - z[..., 16:] * np.sin(pos)[:, None], z[..., :16] * np.sin(pos)[:, None] + z[..., 16:] * np.cos(pos)[:, None]], -1)  # noqa: E731
+        q, k = turn(q), np.repeat(turn(k), 2, 1)
+        s = np.einsum("ihd,jhd->hij", q, k) / np.sqrt(32) + np.where(np.tri(n) > 0, 0.0, -np.inf)
+        p = np.exp(s - s.max(-1, keepdims=True))
+        o.append(np.einsum("hij,jhd->ihd", p / p.sum(-1, keepdims=True), np.repeat(v, 2, 1)).reshape(n, -1))
+        at += n
+    s2 = x64 + np.concatenate(o) @ w[1].T
+    gu = mx.norm(s2, f64(a.norm_feed_forward), a.eps) @ w[2].T
+    want = mx.gated(gu[:, :320], gu[:, 320:]) @ w[3].T
+    assert np.linalg.norm(f64(stream) - s2) <= 2 * 2.0 ** -4 * np.linalg.norm(s2)
+    assert np.linalg.norm(f64(update) - want) <= 4 * 2.0 ** -4 * np.linalg.norm(want)
+
+
+@pytest.mark.gpu
+def test_from_the_last_layer_to_the_tokens():
+    """Norm, logits and choice, eagerly and in a captured graph that is replayed with other rows and numbers."""
+    rows, c, vocab = 5, 256, 1003
+    g = torch.Generator(device="cuda").manual_seed(2)
+    head = dl.Projection(torch.randn((vocab, c), device="cuda", generator=g) * c ** -0.5, bias=torch.randn(vocab, device="cuda", generator=g))
+    weight, x, more, u = torch.ones(c, device="cuda"), *(torch.randn((rows, c), device="cuda", generator=g) for _ in range(2)), torch.rand(rows, device="cuda", generator=g)
+    limit = dict(temperature=torch.tensor([0.0, 0.7, 1.0, 1.3, 1.0], device="cuda"), top_k=torch.tensor([0, 5, 0, 40, 1], dtype=torch.int32, device="cuda"),
+                 top_p=torch.tensor([1.0, 1.0, 0.8, 0.9, 1.0], device="cuda"), min_p=torch.tensor([0.0, 0.0, 0.1, 0.01, 0.0], device="cuda"))
+    choices = [dl.TokenChoice(rows, vocab, torch.float32, **limit) for _ in range(2)]
+
+    def run(choice):
+        logits = head(dl.add_norm(x, more, weight, out="mx8")[1], torch.float32)
+        return (logits, *choice(logits, u))
+
+    run(choices[0])
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        held = run(choices[0])
+    for i in range(4):
+        if i:
+            for v in (x, more):
+                v.copy_(torch.randn((rows, c), device="cuda", generator=g))
+            u.copy_(torch.rand(rows, device="cuda", generator=g))
+        graph.replay()
+        logits, tokens, logs = run(choices[1])
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(held, (logits, tokens, logs)))
+        for r in range(rows):
+            want, wantlog, margin = mx.sample(logits[r].double().cpu().numpy(), uniform=u[r].item(), **{k: v[r].item() for k, v in limit.items()})
+            if margin >= vocab * 2.0 ** -42:
+                assert int(tokens[r]) == want and abs(float(logs[r]) - wantlog) <= 1e-6
+        assert int(tokens[0]) == int(logits[0].argmax()) and int(tokens[4]) == int(logits[4].argmax())
+
+
+@pytest.mark.gpu
+def test_calls_that_are_refused():
+    x = torch.randn((4, 256), device="cuda")
+    p = dl.Projection(torch.randn((40, 256), device="cuda"))
+    for call in (lambda: p(dl.MxMatrix.write(x[:, :200], "mx8"), torch.float32), lambda: dl.add_norm(x, x[:3], torch.ones(256, device="cuda")),
+                 lambda: dl.add_norm(x, x.bfloat16(), torch.ones(256, device="cuda")), lambda: dl.add_norm(x, None, torch.ones(255, device="cuda")),
+                 lambda: dl.add_norm(x, None, torch.ones(256)), lambda: dl.MxMatrix.write(x[:, 1:], "mx8"), lambda: dl.MxMatrix.write(x[:, :255], "mx8", gate=True),
+                 lambda: dl.Projection(torch.randn((40, 256), device="cuda"), bias=torch.zeros(41, device="cuda")),
+                 lambda: dl.TokenChoice(4, 256, torch.float32)(x[:3], torch.zeros(3, device="cuda")), lambda: dl.TokenChoice(4, 256, torch.float32)(x, torch.zeros(3, device="cuda")),
+                 lambda: dl.TokenChoice(4, 256, torch.float32)(x.t().contiguous().t(), torch.zeros(4, device="cuda"))):
+        with pytest.raises(ValueError):
+            call()
+    assert dl.MxMatrix.write(x[:0], "mx4").read(torch.float32).shape == (0, 256)
+    assert p(dl.MxMatrix.write(x[:0], "mx4"), torch.float32).shape == (0, 40)
