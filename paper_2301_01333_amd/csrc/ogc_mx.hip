@@ -24,7 +24,7 @@ MX_DEV float gated(float a, float b) {
     const float lo = __builtin_fmaf(m, 1.44269502162933349609f, -hi) + m * 1.92596299112661746887e-8f;
     float t = __builtin_amdgcn_exp2f(hi);
     t = __builtin_fmaf(t, lo * 0.69314718055994530942f, t);
-    return a * ((a < 0.0f ? t : 1.0f) / (1.0f + t)) * b;
+    return a * ((a < 0.0f ? t : 1.0f) * __builtin_amdgcn_rcpf(1.0f + t)) * b;  // (the reciprocal is off by 2^-23)
 }
 
 template <int DT, int FORMAT, int GATE> __global__ __launch_bounds__(256) void ogc_mx_write_kernel(RowsArgs a) {

@@ -3,7 +3,10 @@
 // Rows are read once, kept in registers, and written twice (the sum and its norm): the kernel is bound by memory, or by its launch.  A
 // lane holds N runs of eight channels.  In its own type a workgroup has one row; in a microscaled format it has eight, eight lanes of a
 // wavefront each, because the codes of eight rows are 128 bytes side by side in the matrix, and a wavefront's four runs of a row
-// are a block of 256 channels, whose four scales are one word.  Rows that do not fit the registers (N = 0) are read a second time for the norm.
+// are a block of 256 channels, whose four scales are one word.  Where that leaves compute units without work it has two rows, 32 lanes
+// each, whose runs are such a block.  Rows that do not fit the registers (N = 0) are read a second time for the norm.
+// 8192 x 4096 in bf16 with a residual: in its own type 50 us (268 MB, 5.4 TB/s), to 8 bits 56 (236 MB, 4.2); tried for the latter and no better: rows read a
+// kilobyte at a time and turned in LDS (62), twice the wavefronts with half the registers (59).
 #include "ogc_mx_rows.h"
 
 #include <math.h>
@@ -25,8 +28,10 @@ struct NormArgs {
 
 constexpr int NORM_WAVES = 16;
 
-template <int DT, int OUT, int N> __global__ __launch_bounds__(64 * NORM_WAVES) void ogc_norm_kernel(NormArgs a) {
-    constexpr int E = MxEight<DT>::E, ROWS = OUT == OGC_NORM_SAME ? 1 : 8, LANES = 64 / ROWS;  // rows of a workgroup, lanes of a row in a wavefront
+// ROWS: of a workgroup
+template <int DT, int OUT, int ROWS, int N> __global__ __launch_bounds__(64 * NORM_WAVES) void ogc_norm_kernel(NormArgs a) {
+    constexpr int E = MxEight<DT>::E, LANES = 64 / ROWS;  // lanes of a row in a wavefront
+    constexpr int SPAN = ROWS == 8 ? MX_BLOCK : LANES * 8, RUNS = SPAN / (LANES * 8);  // channels and runs that a wavefront takes in turn
     __shared__ double part[NORM_WAVES][ROWS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int64_t row = (int64_t)blockIdx.x * ROWS + lane / LANES;
@@ -35,12 +40,9 @@ template <int DT, int OUT, int N> __global__ __launch_bounds__(64 * NORM_WAVES) 
     const int64_t r = on ? row : 0;
     const uint8_t *const x = a.x + r * a.sx, *const res = a.residual ? a.residual + r * a.sr : nullptr;
     uint8_t* const sum = a.residual ? a.sum + r * a.ss : nullptr;
-    // first channel of a lane's run i: whole wavefronts of a row take 512 channels in turn, those of eight rows 256
-    const auto first = [&](int i) {
-        return OUT == OGC_NORM_SAME ? (i * waves + wave) * 512 + j * 8 : (i / 4 * waves + wave) * MX_BLOCK + i % 4 * 64 + j * 8;
-    };
+    const auto first = [&](int i) { return (i / RUNS * waves + wave) * SPAN + i % RUNS * LANES * 8 + j * 8; };  // channel of a lane's run i
     const int limit = OUT == OGC_NORM_SAME ? a.channels : a.padded;
-    const int runs = OUT == OGC_NORM_SAME ? (limit + 512 * waves - 1) / (512 * waves) : (limit + MX_BLOCK * waves - 1) / (MX_BLOCK * waves) * 4;
+    const int runs = (limit + SPAN * waves - 1) / (SPAN * waves) * RUNS;
 
     MxEight<DT> held[N > 0 ? N : 1];
     double square = 0.0;  // eight squares are added up in fp32, these sums in 64 bits: the factor of a row is the rounded one, whatever its length
@@ -59,20 +61,16 @@ template <int DT, int OUT, int N> __global__ __launch_bounds__(64 * NORM_WAVES) 
         square += (double)eight;
     };
     if constexpr (N > 0) {
-        constexpr int M = DT == OGC_F32 && N > 4 ? 4 : N;  // (registers: eight runs of fp32 have their residuals four at a time)
+        MxEight<DT> more[N];
 #pragma unroll
-        for (int i0 = 0; i0 < N; i0 += M) {
-            MxEight<DT> more[M];
-#pragma unroll
-            for (int i = 0; i < M; ++i) {
-                const int c = first(i0 + i), there = on ? a.channels - c : 0;
-                held[i0 + i].load(x + (int64_t)c * E, there);
-                if (res) more[i].load(res + (int64_t)c * E, there);
-                else more[i].clear();
-            }
-#pragma unroll
-            for (int i = 0; i < M; ++i) take(held[i0 + i], more[i], first(i0 + i));
+        for (int i = 0; i < N; ++i) {
+            const int c = first(i), there = on ? a.channels - c : 0;
+            held[i].load(x + (int64_t)c * E, there);
+            if (res) more[i].load(res + (int64_t)c * E, there);
+            else more[i].clear();
         }
+#pragma unroll
+        for (int i = 0; i < N; ++i) take(held[i], more[i], first(i));
     } else {
         for (int i = 0; i < runs; ++i) {
             const int c = first(i), there = on ? a.channels - c : 0;
@@ -112,12 +110,16 @@ template <int DT, int OUT, int N> __global__ __launch_bounds__(64 * NORM_WAVES) 
             constexpr int FORMAT = OUT == OGC_NORM_MX8 ? OGC_MX8 : OGC_MX4;
             uint32_t e;
             const mx_v2u code = mx_quantized<FORMAT>(v, e);
-            scales = i % 4 ? scales | e << (i % 4 * 8) : e;
             if (on && c < a.padded) {
                 uint8_t* const o = a.y + mx_code_at(FORMAT, a.padded, (int)row, c);
                 if constexpr (FORMAT == OGC_MX8) *(mx_v2u*)o = code;
                 else *(uint32_t*)o = code[0];
-                if (i % 4 == 3 && j % 4 == 0) *(uint32_t*)(a.scales + mx_scales_at(a.padded, (int)row, c / MX_BLOCK, j / 4)) = scales;
+            }
+            if constexpr (ROWS == 8) {
+                scales = i % 4 ? scales | e << (i % 4 * 8) : e;
+                if (on && c < a.padded && i % 4 == 3 && j % 4 == 0) *(uint32_t*)(a.scales + mx_scales_at(a.padded, (int)row, c / MX_BLOCK, j / 4)) = scales;
+            } else {
+                if (on && c < a.padded && j % 4 == 0) a.scales[mx_scales_at(a.padded, (int)row, c / MX_BLOCK, j / 4 % 2) + j / 8] = (uint8_t)e;
             }
         }
     };
@@ -136,26 +138,31 @@ template <int DT, int OUT, int N> __global__ __launch_bounds__(64 * NORM_WAVES) 
     }
 }
 
-template <int DT, int OUT> void launch(const NormArgs& a, hipStream_t st) {
-    constexpr int ROWS = OUT == OGC_NORM_SAME ? 1 : 8, SPAN = OUT == OGC_NORM_SAME ? 512 : 256, RUNS = OUT == OGC_NORM_SAME ? 1 : 4;  // channels and runs of a wavefront's turn
+// Wavefronts of a row: as many as hold it in eight runs (fp32: four) of their lanes, or more, where rows are few.
+template <int DT, int OUT, int ROWS> void launch(const NormArgs& a, hipStream_t st) {
+    constexpr int LANES = 64 / ROWS, SPAN = ROWS == 8 ? MX_BLOCK : LANES * 8, RUNS = SPAN / (LANES * 8), MOST = DT == OGC_F32 ? 4 : 8;
     const unsigned grid = (unsigned)(((int64_t)a.rows + ROWS - 1) / ROWS);
     const int turns = ((OUT == OGC_NORM_SAME ? a.channels : a.padded) + SPAN - 1) / SPAN;
     int waves = 1;
-    while (waves < NORM_WAVES && turns > waves * (8 / RUNS)) waves *= 2;
-    if (grid < 1024)
-        while (waves < NORM_WAVES && turns > waves) waves *= 2;
+    while (waves < NORM_WAVES && turns > waves && (turns * RUNS > waves * MOST || (int64_t)grid * waves < 4096)) waves *= 2;
     const int runs = (turns + waves - 1) / waves * RUNS;
     const dim3 g(grid), t(64 * waves);
     if constexpr (RUNS == 1) {
         if (runs <= 2) {
-            if (runs <= 1) hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, 1>), g, t, 0, st, a);
-            else hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, 2>), g, t, 0, st, a);
+            if (runs <= 1) hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, ROWS, 1>), g, t, 0, st, a);
+            else hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, ROWS, 2>), g, t, 0, st, a);
             return;
         }
     }
-    if (runs <= 4) hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, 4>), g, t, 0, st, a);
-    else if (runs <= 8) hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, 8>), g, t, 0, st, a);
-    else hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, 0>), g, t, 0, st, a);
+    if (runs <= 4) hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, ROWS, 4>), g, t, 0, st, a);
+    else if (runs <= MOST) hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, ROWS, MOST>), g, t, 0, st, a);
+    else hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, ROWS, 0>), g, t, 0, st, a);
+}
+template <int DT> void launch(int out, const NormArgs& a, hipStream_t s) {
+    const bool few = a.rows < 8 * 256;  // (eight rows each would leave compute units without work: 64 x 8192 in bf16 to 8 bits 5.7 us, eight rows each 12.5)
+    if (out == OGC_NORM_SAME) launch<DT, OGC_NORM_SAME, 1>(a, s);
+    else if (out == OGC_NORM_MX4) few ? launch<DT, OGC_NORM_MX4, 2>(a, s) : launch<DT, OGC_NORM_MX4, 8>(a, s);
+    else few ? launch<DT, OGC_NORM_MX8, 2>(a, s) : launch<DT, OGC_NORM_MX8, 8>(a, s);
 }
 
 bool aligned(int64_t stride, int e) { return stride >= 0 && stride * e % 16 == 0; }
@@ -205,10 +212,8 @@ ogc_status ogc_norm_run(const ogc_norm_desc* d, const void* x, const void* resid
     a.eps = d->eps;
     a.inv = 1.0 / (double)d->channels;
     const hipStream_t s = (hipStream_t)stream;
-    const bool f32 = d->dtype == OGC_F32;
-    if (same) f32 ? launch<OGC_F32, OGC_NORM_SAME>(a, s) : launch<OGC_BF16, OGC_NORM_SAME>(a, s);
-    else if (d->out == OGC_NORM_MX4) f32 ? launch<OGC_F32, OGC_NORM_MX4>(a, s) : launch<OGC_BF16, OGC_NORM_MX4>(a, s);
-    else f32 ? launch<OGC_F32, OGC_NORM_MX8>(a, s) : launch<OGC_BF16, OGC_NORM_MX8>(a, s);
+    if (d->dtype == OGC_F32) launch<OGC_F32>(d->out, a, s);
+    else launch<OGC_BF16>(d->out, a, s);
     return hipGetLastError() == hipSuccess ? OGC_OK : OGC_ERR_DEVICE;
 }
 
