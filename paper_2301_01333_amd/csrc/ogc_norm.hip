@@ -5,8 +5,9 @@
 // wavefront each, because the codes of eight rows are 128 bytes side by side in the matrix, and a wavefront's four runs of a row
 // are a block of 256 channels, whose four scales are one word.  Where that leaves compute units without work it has two rows, 32 lanes
 // each, whose runs are such a block.  Rows that do not fit the registers (N = 0) are read a second time for the norm.
-// 8192 x 4096 in bf16 with a residual: in its own type 50 us (268 MB, 5.4 TB/s), to 8 bits 56 (236 MB, 4.2); tried for the latter and no better: rows read a
-// kilobyte at a time and turned in LDS (62), twice the wavefronts with half the registers (59).
+// 8192 x 4096 in bf16 with a residual: in its own type 49 us (268 MB, 5.5 TB/s), to 8 bits 57 (236 MB, 4.1: the reads of eight rows and the codes' 128 bytes
+// cost what they save).  Many wavefronts with few runs each: eight runs a lane 56 and 63; tried for 8 bits and no better: rows read a kilobyte at
+// a time and turned in LDS (62).
 #include "ogc_mx_rows.h"
 
 #include <math.h>
@@ -34,7 +35,9 @@ template <int DT, int OUT, int ROWS, int N> __global__ __launch_bounds__(64 * NO
     constexpr int SPAN = ROWS == 8 ? MX_BLOCK : LANES * 8, RUNS = SPAN / (LANES * 8);  // channels and runs that a wavefront takes in turn
     __shared__ double part[NORM_WAVES][ROWS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-    const int64_t row = (int64_t)blockIdx.x * ROWS + lane / LANES;
+    // (eight rows: workgroup i runs on XCD i % 8, and the four workgroups of 32 rows of the matrix shall be one XCD's)
+    const uint32_t group = ROWS == 8 ? blockIdx.x / 32 * 32 + blockIdx.x % 8 * 4 + blockIdx.x / 8 % 4 : blockIdx.x;
+    const int64_t row = (int64_t)group * ROWS + lane / LANES;
     const int j = lane % LANES;
     const bool on = row < a.rows;
     const int64_t r = on ? row : 0;
@@ -138,10 +141,10 @@ template <int DT, int OUT, int ROWS, int N> __global__ __launch_bounds__(64 * NO
     }
 }
 
-// Wavefronts of a row: as many as hold it in eight runs (fp32: four) of their lanes, or more, where rows are few.
+// Wavefronts of a row: as many as hold it in two runs (of eight rows: four) of their lanes, or more, where rows are few.
 template <int DT, int OUT, int ROWS> void launch(const NormArgs& a, hipStream_t st) {
-    constexpr int LANES = 64 / ROWS, SPAN = ROWS == 8 ? MX_BLOCK : LANES * 8, RUNS = SPAN / (LANES * 8), MOST = DT == OGC_F32 ? 4 : 8;
-    const unsigned grid = (unsigned)(((int64_t)a.rows + ROWS - 1) / ROWS);
+    constexpr int LANES = 64 / ROWS, SPAN = ROWS == 8 ? MX_BLOCK : LANES * 8, RUNS = SPAN / (LANES * 8), MOST = ROWS == 8 ? 4 : 2;
+    const unsigned grid = (unsigned)(ROWS == 8 ? ((int64_t)a.rows + 255) / 256 * 32 : ((int64_t)a.rows + ROWS - 1) / ROWS);
     const int turns = ((OUT == OGC_NORM_SAME ? a.channels : a.padded) + SPAN - 1) / SPAN;
     int waves = 1;
     while (waves < NORM_WAVES && turns > waves && (turns * RUNS > waves * MOST || (int64_t)grid * waves < 4096)) waves *= 2;
@@ -155,7 +158,7 @@ template <int DT, int OUT, int ROWS> void launch(const NormArgs& a, hipStream_t 
         }
     }
     if (runs <= 4) hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, ROWS, 4>), g, t, 0, st, a);
-    else if (runs <= MOST) hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, ROWS, MOST>), g, t, 0, st, a);
+    else if (DT == OGC_BF16 && runs <= 8) hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, ROWS, 8>), g, t, 0, st, a);
     else hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, ROWS, 0>), g, t, 0, st, a);
 }
 template <int DT> void launch(int out, const NormArgs& a, hipStream_t s) {
