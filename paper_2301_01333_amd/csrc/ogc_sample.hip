@@ -86,11 +86,10 @@ struct Weights {
         return __builtin_bit_cast(uint64_t, __builtin_bit_cast(double, bits) + 0x1p52) & 0xfffffffffffffull;
     }
     static __device__ __forceinline__ uint64_t of_log(double x) { return of_log2(x * 1.44269504088896340736); }
-    // of a logit, which is at most the largest: the same instructions wherever a part's weights are added up
-    __device__ __forceinline__ uint64_t of_part(float logit) const {
-        const double x = logit;
-        return of_log2(x == largest ? 0.0 : (x - largest) * (per * 1.44269504088896340736));
-    }
+    // of a logit, which is at most the largest (or NaN: none), where that is finite: the same instructions wherever a part's weights are added up
+    __device__ __forceinline__ uint64_t of_part(float logit) const { return of_log2(((double)logit - largest) * (per * 1.44269504088896340736)); }
+    // where it is plus infinity
+    static __device__ __forceinline__ uint64_t of_infinite(float logit) { return logit == INFINITY ? 1ull << 42 : 0; }
     __device__ __forceinline__ uint64_t of(uint32_t key) const { return key == NOTHING ? 0 : of_log(log_of(logit_of(key))); }
 };
 
@@ -349,6 +348,7 @@ template <int DT, int RUNS> __global__ __launch_bounds__(SCAN_THREADS) void ogc_
     weights.largest = top;
     weights.per = l.per;
     const float high = place_of(top, l.fine);
+    const bool infinite = top == INFINITY;
     uint64_t sum = 0;
 #pragma unroll 1
     for (int i = 0; i < RUNS; ++i) {  // (read once more, from the caches: with all of them unrolled the code takes longer to come than the exponentials)
@@ -356,8 +356,8 @@ template <int DT, int RUNS> __global__ __launch_bounds__(SCAN_THREADS) void ogc_
         y.load(row, first + i * SCAN_THREADS * 8 - off, a.vocab);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float v = y.number(e);
-            const uint64_t w = weights.of_part(v);
+            const float v = y.get(e);
+            const uint64_t w = infinite ? Weights::of_infinite(v) : weights.of_part(v);
             sum += w;
             if (fill && w) {
                 const float d = high - place_of(v, l.fine);
@@ -403,39 +403,56 @@ SAMPLE_DEV uint64_t sum_before(uint64_t x, uint64_t* part, uint64_t& all) {
     all = lane_of(w, WAVES - 1);
     return (wave ? lane_of(w, wave - 1) : 0) + s - x;
 }
-// Sorts n different tokens, falling.  Up to 1024, a thread each: by the upper 32 bits into 1024 bins of equal width, and within a bin by counting the larger
-// ones.  More of them, or many in a bin: by halves, where pairs up to 64 apart are one wavefront's.
-SAMPLE_DEV void sort(Chosen& sh, int n, uint32_t least, uint32_t most) {  // the least and the largest that the upper 32 bits may be
-    uint64_t* const v = sh.tokens;
-    if (n <= THREADS) {
-        const bool on = (int)threadIdx.x < n;
-        const uint64_t own = on ? v[threadIdx.x] : 0;
-        sh.counts[threadIdx.x] = 0;
-        if (threadIdx.x == 0) sh.crowded = 0;
-        __syncthreads();
-        const float scale = 1023.0f / (float)max(most - least, 1u);
-        const int bin = min((int)((float)(most - (uint32_t)(own >> 32)) * scale), FINE - 1);
-        uint32_t slot = 0;
-        if (on) slot = atomicAdd(&sh.counts[bin], 1u);
-        if (on && slot >= 48) sh.crowded = 1;
-        __syncthreads();
-        if (!sh.crowded) {
-            uint64_t all;
-            const uint32_t start = (uint32_t)sum_before(sh.counts[threadIdx.x], sh.part, all);
-            sh.starts[threadIdx.x] = start;
-            __syncthreads();
-            const uint32_t from = on ? sh.starts[bin] : 0, count = on ? sh.counts[bin] : 0;
-            if (on) v[from + slot] = own;
-            __syncthreads();
-            uint32_t larger = 0;
-            for (uint32_t j = 0; j < count; ++j) larger += v[from + j] > own;
-            __syncthreads();
-            if (on) v[from + larger] = own;
-            __syncthreads();
-            return;
-        }
-        __syncthreads();
+// Sorts n different tokens, falling: into 1024 bins of equal width by value(token), which orders them the same way and is below `range`, and within a bin
+// by counting the larger ones.  EACH: tokens of a thread; false: too many in a bin.
+template <int EACH, class V> SAMPLE_DEV bool sort_by_bins(Chosen& sh, int n, V value, uint64_t range) {
+    uint64_t *const v = sh.tokens, own[EACH];
+    uint32_t slot[EACH];
+    int bin[EACH];
+    sh.counts[threadIdx.x] = 0;
+    if (threadIdx.x == 0) sh.crowded = 0;
+    const float scale = 1023.0f / (float)range;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        const int i = threadIdx.x + e * THREADS;
+        own[e] = i < n ? v[i] : 0;
+        bin[e] = i < n ? min((int)((float)(range - 1 - value(own[e])) * scale), FINE - 1) : 0;
     }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
+        if ((int)threadIdx.x + e * THREADS < n) {
+            slot[e] = atomicAdd(&sh.counts[bin[e]], 1u);
+            if (slot[e] >= 48) sh.crowded = 1;
+        }
+    __syncthreads();
+    if (sh.crowded) return false;
+    uint64_t all;
+    sh.starts[threadIdx.x] = (uint32_t)sum_before(sh.counts[threadIdx.x], sh.part, all);
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
+        if ((int)threadIdx.x + e * THREADS < n) v[sh.starts[bin[e]] + slot[e]] = own[e];
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
+        if ((int)threadIdx.x + e * THREADS < n) {
+            const uint32_t from = sh.starts[bin[e]], count = sh.counts[bin[e]];
+            slot[e] = from;
+            for (uint32_t j = 0; j < count; ++j) slot[e] += v[from + j] > own[e];
+        }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
+        if ((int)threadIdx.x + e * THREADS < n) v[slot[e]] = own[e];
+    __syncthreads();
+    return true;
+}
+// The same whatever their bins: then by halves, where pairs up to 64 apart are one wavefront's.
+template <class V> SAMPLE_DEV void sort(Chosen& sh, int n, V value, uint64_t range) {
+    if (n <= THREADS ? sort_by_bins<1>(sh, n, value, range) : sort_by_bins<MOST / THREADS>(sh, n, value, range)) return;
+    __syncthreads();
+    uint64_t* const v = sh.tokens;
     int to = 64;
     while (to < n) to *= 2;
     for (int i = n + threadIdx.x; i < to; i += THREADS) v[i] = 0;  // zeros sort last
@@ -544,14 +561,21 @@ template <int DT> SAMPLE_DEV void collect(const SampleArgs& a, Chosen& sh, const
     const float* const tops = a.tops + (int64_t)blockIdx.x * a.chunks;
     const int off = off_of<DT>(row);
     low = fmaxf(low, -3.4028234663852886e38f);  // (minus infinity is no token)
+    float after[AHEAD];
+    const auto look = [&](int i0) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) after[u] = tops[min(i0 + u * THREADS, a.chunks - 1)];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) after[u] = i0 + u * THREADS < a.chunks ? after[u] : -INFINITY;
+    };
+    look(threadIdx.x);
 #pragma unroll 1
     for (int i0 = threadIdx.x; i0 < a.chunks; i0 += AHEAD * THREADS) {
         float m[AHEAD];
         Eight<DT> x[AHEAD];
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) m[u] = tops[min(i0 + u * THREADS, a.chunks - 1)];
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) m[u] = i0 + u * THREADS < a.chunks ? m[u] : -INFINITY;
+        for (int u = 0; u < AHEAD; ++u) m[u] = after[u];
+        look(i0 + AHEAD * THREADS);
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int i = (i0 + u * THREADS) * 8 - off;
@@ -608,11 +632,19 @@ SAMPLE_DEV uint64_t goal_of(double p, uint64_t all) {
     return goal ? goal : 1;
 }
 
+// Sorts tokens whose keys are from least to most by their logits, the lowest index first of equal ones: by logit and index together, counted in the steps that
+// the type has, so that equal logits (in bf16 there are many) do not share a bin.
+template <int DT> SAMPLE_DEV void sort_by_logit(Chosen& sh, int n, int vocab, uint32_t least, uint32_t most) {
+    constexpr int STEP = DT == OGC_F32 ? 0 : 16;
+    sort(sh, n, [&](uint64_t t) { return (uint64_t)((key_in(t) >> STEP) - (least >> STEP)) * vocab + (vocab - 1 - index_in(t)); },
+         (uint64_t)((most >> STEP) - (least >> STEP) + 1) * vocab);
+}
+
 // The choice among the first n <= 1024 tokens, which become sorted by index.
 SAMPLE_DEV Result choose(Chosen& sh, int n, int vocab, const Weights& weights, float u) {
     if ((int)threadIdx.x < n) sh.tokens[threadIdx.x] = sh.tokens[threadIdx.x] << 32 | sh.tokens[threadIdx.x] >> 32;  // the index's complement first: falling is the lowest index first
     __syncthreads();
-    sort(sh, n, ~(uint32_t)(vocab - 1), ~0u);
+    sort(sh, n, [&](uint64_t t) { return (uint64_t)((uint32_t)(t >> 32) + (uint32_t)vocab); }, (uint64_t)vocab);  // (~index + vocab)
     const uint64_t mine = (int)threadIdx.x < n ? sh.tokens[threadIdx.x] : 0;
     const double x = (int)threadIdx.x < n ? weights.log_of(logit_of((uint32_t)mine)) : -INFINITY;
     const uint64_t w = Weights::of_log(x);
@@ -681,7 +713,7 @@ template <int DT> SAMPLE_DEV bool by_top_k(const SampleArgs& a, Chosen& sh, cons
     int n = (int)sh.count;
     __syncthreads();
     if (n > MOST) return false;
-    sort(sh, n, min(low, key_of(logit_of(low))), key_of((float)weights.largest));
+    sort_by_logit<DT>(sh, n, a.vocab, min(low, key_of(logit_of(low))), key_of((float)weights.largest));
     n = min(n, l.k);
     if (l.top_p || l.min_p) {
         sum_before((int)threadIdx.x < n ? weights.of(key_in(sh.tokens[threadIdx.x])) : 0, sh.part, all);
@@ -749,7 +781,7 @@ template <int DT> SAMPLE_DEV bool by_parts(const SampleArgs& a, Chosen& sh, cons
         const int n = (int)sh.count;
         __syncthreads();
         if (n > MOST) return false;
-        sort(sh, n, min(low, key_of(logit_of(low))), max(behind, key_of(logit_of(behind))));
+        sort_by_logit<DT>(sh, n, a.vocab, min(low, key_of(logit_of(low))), max(behind, key_of(logit_of(behind))));
         kept = n <= THREADS ? kept_of<1>(sh, n, weights, l, before, goal) : kept_of<MOST / THREADS>(sh, n, weights, l, before, goal);
     }
     // ---- the part that has the token: what is kept of each
@@ -786,12 +818,13 @@ template <int DT> SAMPLE_DEV bool by_parts(const SampleArgs& a, Chosen& sh, cons
     else x.clear();
     const auto weight = [&](float v, int e) -> uint64_t {
         const uint64_t token = (uint64_t)key_of(v) << 32 | (uint32_t)~(uint32_t)(at + e);
-        return v > -INFINITY && (!limited || away(v) < (float)from || token >= end) ? near.of_part(v) : 0;
+        if (!(v > -INFINITY) || (limited && !(away(v) < (float)from) && token < end)) return 0;
+        return near.largest == INFINITY ? Weights::of_infinite(v) : near.of_part(v);
     };
     uint64_t mine = 0, all;
-#pragma unroll 1
+#pragma unroll 4
     for (int e = 0; e < 8; ++e) {
-        mine += weight(x.number(0), e);
+        mine += weight(x.get(0), e);
         x.next();
     }
     run = sum_before(mine, sh.part, all);
@@ -799,9 +832,9 @@ template <int DT> SAMPLE_DEV bool by_parts(const SampleArgs& a, Chosen& sh, cons
     if (run <= goal && goal < run + mine) {
 #pragma unroll 1
         for (int e = 0; e < 8; ++e) {
-            const uint64_t w = weight(x.number(0), e);
+            const uint64_t w = weight(x.get(0), e);
             if (goal < run + w) {
-                found = {at + e, weights.log_of(x.number(0)), total};
+                found = {at + e, weights.log_of(x.get(0)), total};
                 break;
             }
             run += w;
