@@ -18,9 +18,10 @@ struct RowsArgs {
     int even;          // gate: the second halves of the rows are 16-byte aligned, too
 };
 
-// a * b / (1 + exp(-a)).  exp(-|a|) neither overflows nor loses what the product of |a| and log2(e) is rounded by.
+// a * b / (1 + exp(-a)).  exp(-|a|) neither overflows nor loses what the product of |a| and log2(e) is rounded by (from |a| = 104 on it is 0 in fp32, and from
+// 2.3e38 on that product would be an infinity).
 MX_DEV float gated(float a, float b) {
-    const float m = -__builtin_fabsf(a), hi = m * 1.44269502162933349609f;
+    const float m = __builtin_fmaxf(-__builtin_fabsf(a), -128.0f), hi = m * 1.44269502162933349609f;
     const float lo = __builtin_fmaf(m, 1.44269502162933349609f, -hi) + m * 1.92596299112661746887e-8f;
     float t = __builtin_amdgcn_exp2f(hi);
     t = __builtin_fmaf(t, lo * 0.69314718055994530942f, t);

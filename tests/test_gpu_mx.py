@@ -219,6 +219,24 @@ def test_gated_rows(fmt, dtype, n, c):
     check_rounded(fmt, gotc, gote, y, 2.0 ** -21 * np.abs(y), c)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gate_of_the_largest_numbers(dtype):
+    """|a| log2(e) is no fp32 number from |a| = 2.36e38 on; a * b / (1 + exp(-a)) is: a * b, or nothing."""
+    x = np.zeros((2, 512))
+    x[0, :256:4], x[1, :256:4] = 3.3e38, -3.3e38
+    x[:, 1:256:4] = 2.0 ** 127
+    x[:, 2:256:4] = -(2.0 ** 100)
+    x[:, 3:256:4] = -88.0
+    x[:, 256:] = np.random.default_rng(3).uniform(-0.5, 0.5, (2, 256)) * np.exp2(-np.repeat(np.arange(0, 128, 16), 32) / 4)
+    v, x64 = device_rows(x, dtype)
+    codes, scales, nc, ns = matrix_buffers("mx8", 2, 256)
+    binding.ogc_mx_write(binding.mx_rows(binding.DTYPES[dtype], 1, 2, 256, 1, v.stride(0)), v.data_ptr(), codes.data_ptr(), scales.data_ptr(), stream())
+    y = mx.gated(x64[:, :256], x64[:, 256:])
+    gotc, gote = mx.codes_of(codes.cpu().numpy()[:nc], scales.cpu().numpy()[:ns], 2, 256, 1)
+    assert (gote < 255).all()
+    check_rounded("mx8", gotc, gote, y, 2.0 ** -21 * np.abs(y), 256)
+
+
 def test_gate_of_what_is_no_number():
     x = np.zeros((1, 512))
     x[0, :256] = 1.0
@@ -416,3 +434,68 @@ def test_product_in_a_graph_and_on_a_stream_of_its_own():
         run(eager)
         torch.cuda.synchronize()
         assert torch.equal(y, eager) and not (y == 3.0).all()
+
+
+@pytest.mark.parametrize("out", ["same", "mx8"])
+def test_norm_beyond_4_gib(out):
+    """Rows, and codes, that begin beyond 2^32 bytes."""
+    torch = torch_()
+    n, c = (1 << 18) + 3, 1 << 14
+    x = torch.zeros((n, c), dtype=torch.bfloat16, device="cuda")
+    last = torch.from_numpy(np.random.default_rng(2).normal(size=(3, c))).to(torch.bfloat16).cuda()
+    x[-3:] = last
+    weight, y = torch.ones(c, device="cuda"), torch.empty((n, c), dtype=torch.bfloat16, device="cuda")
+    codes, scales = binding.ogc_mx_bytes(1, n, c)
+    assert codes > 1 << 32
+    cb, sb = (torch.zeros(k, dtype=torch.uint8, device="cuda") for k in (codes, scales))
+    d = binding.norm_desc(binding.OGC_BF16, n, c, int(out == "mx8") * 2, 0.0, c, 0, 0, c)
+    binding.ogc_norm_run(d, x.data_ptr(), 0, weight.data_ptr(), 0, y.data_ptr() if out == "same" else cb.data_ptr(), sb.data_ptr() if out != "same" else 0, stream())
+    want = mx.norm(last.double().cpu().numpy(), 1.0, 0.0)
+    if out != "same":
+        binding.ogc_mx_read(binding.mx_rows(binding.OGC_BF16, 1, n, c, 0, c), cb.data_ptr(), sb.data_ptr(), y.data_ptr(), stream())
+        top = np.repeat(np.abs(want).reshape(3, -1, 32).max(-1), 32, 1)
+        inside(y[-3:], want, np.abs(want) * (2.0 ** -4 + 2.0 ** -20) + top * 2.0 ** -17, "last rows")
+    else:
+        inside(y[-3:], want, np.abs(want) * (2.0 ** -8 + 2.0 ** -20), "last rows")
+
+
+@pytest.mark.parametrize("m,n,k", [(2, (1 << 18) + 70, 1 << 15), ((1 << 15) + 5, (1 << 15) + 256, 64)])
+def test_products_beyond_4_gib(m, n, k):
+    """Weights, or results, that begin beyond 2^32 bytes; the others are zeros."""
+    torch = torch_()
+    rng = np.random.default_rng(k)
+    at = 33  # so many last rows of both
+    xv, wv = (torch.zeros((r, k), dtype=torch.bfloat16, device="cuda") for r in (m, n))
+    for v in (xv, wv):
+        v[-at:] = torch.from_numpy(rng.normal(size=(min(at, v.shape[0]), k))).to(torch.bfloat16).cuda()
+    mats = []
+    for v, fmt in ((xv, 1), (wv, 0)):
+        codes, scales = (torch.zeros(s, dtype=torch.uint8, device="cuda") for s in binding.ogc_mx_bytes(fmt, *v.shape))
+        binding.ogc_mx_write(binding.mx_rows(binding.OGC_BF16, fmt, *v.shape, 0, k), v.data_ptr(), codes.data_ptr(), scales.data_ptr(), stream())
+        mats.append((codes, scales, mx.values(*mx.quantize(v[-at:].double().cpu().numpy(), fmt), fmt)))
+    (x, xs, x64), (w, ws, w64) = mats
+    assert w.numel() > 1 << 32 or m * n * 4 > 1 << 32
+    wide = mx.up(n, 4) + 4
+    y = torch.full((m, wide), 5.0, device="cuda")
+    binding.ogc_mx_product_run(binding.mx_product_desc(binding.OGC_F32, 1, 0, m, n, k, 0, wide), x.data_ptr(), xs.data_ptr(), w.data_ptr(), ws.data_ptr(), 0, y.data_ptr(), 0, stream())
+    # (an instruction's 64 products: each 2^-13 of the largest at most; sums of k / 64 of them)
+    tol = k * 2.0 ** -13 * np.abs(x64).max(1)[:, None] * np.abs(w64).max(1)[None, :] + (k / 64 + 8) * 2.0 ** -24 * (np.abs(x64) @ np.abs(w64).T)
+    inside(y[-at:, n - at:n], x64 @ w64.T, tol, "last ones")
+    assert not y[:-at, :n].any() and not y[-at:, :n - at].any() and bool((y[:, n:] == 5.0).all())
+
+
+def test_products_at_once_on_two_streams():
+    torch = torch_()
+    rng = np.random.default_rng(12)
+    m, n, k = 1400, 1300, 1000
+    mats = [mx.matrix(rng.normal(size=s), 0) for s in ((m, k), (n, k))]
+    (x, xs), (w, ws) = ([torch.from_numpy(t).cuda() for t in v] for v in mats)
+    desc = binding.mx_product_desc(1, 0, 0, m, n, k, 0, 1304)
+    ys = [torch.zeros((m, 1304), dtype=torch.bfloat16, device="cuda") for _ in range(5)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for i, y in enumerate(ys[1:]):
+        binding.ogc_mx_product_run(desc, x.data_ptr(), xs.data_ptr(), w.data_ptr(), ws.data_ptr(), 0, y.data_ptr(), 0, int(streams[i % 2].cuda_stream))
+    torch.cuda.synchronize()
+    binding.ogc_mx_product_run(desc, x.data_ptr(), xs.data_ptr(), w.data_ptr(), ws.data_ptr(), 0, ys[0].data_ptr(), 0, stream())
+    assert ys[0].any() and all(torch.equal(y, ys[0]) for y in ys[1:])

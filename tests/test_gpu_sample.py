@@ -151,6 +151,24 @@ def test_strides_and_offsets(dtype):
     assert np.array_equal(a, b)
 
 
+def test_rows_beyond_4_gib():
+    torch = torch_()
+    rng = np.random.default_rng(8)
+    rows, vocab, stride = 3, 5000, (1 << 30) + 1
+    flat = torch.empty((rows - 1) * stride + vocab, device="cuda")
+    x = flat.as_strided((rows, vocab), (stride, 1))
+    x.copy_(torch.from_numpy(some(rng, rows, vocab)))
+    near = x.contiguous()
+    u, k, share = torch.tensor([0.1, 0.5, 0.9], device="cuda"), torch.tensor([0, 30, 0], dtype=torch.int32, device="cuda"), torch.tensor([1.0, 0.9, 0.7], device="cuda")
+    tokens = []
+    for v, s in ((x, stride), (near, vocab)):
+        desc = binding.sample_desc(0, rows, vocab, s)
+        space, token = torch.empty(binding.ogc_sample_workspace_bytes(desc), dtype=torch.uint8, device="cuda"), torch.full((rows,), -7, dtype=torch.int32, device="cuda")
+        binding.ogc_sample_run(desc, v.data_ptr(), 0, k.data_ptr(), share.data_ptr(), 0, u.data_ptr(), token.data_ptr(), 0, space.data_ptr(), stream())
+        tokens.append(token.tolist())
+    assert tokens[0] == tokens[1]
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("sigma,temperature", [(0.02, 1.0), (1.0, 0.05), (2.0, 1.5), (40.0, 1.0), (300.0, 30.0), (1e30, 1.0), (1e-30, 1e-28)])
 def test_spreads(dtype, sigma, temperature):
