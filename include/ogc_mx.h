@@ -17,6 +17,7 @@
  * rounded up are left as they were, and no result depends on them.  ogc_mx_bytes gives the sizes; codes and scales are 16-byte aligned.
  *
  * Other tensors are DEVICE pointers to rows of contiguous channels, a stride apart (in elements; a multiple of 16 bytes; bases 16-byte aligned).
+ * Rows that are read may overlap (a stride of 0 is the same row again), rows that are written must not.
  * Types: OGC_F32 and OGC_BF16.  Sums and norms are held in 32 bits; results are rounded once, to nearest even.
  *
  * Every call is asynchronous on `stream` (a hipStream_t, NULL = the default stream) and may be captured into a graph; the library
@@ -41,7 +42,8 @@ ogc_status ogc_mx_bytes(int32_t format, int32_t rows, int32_t channels, size_t* 
 /* ---- the residual's addition with the root-mean-square norm ----------------------------------------------------------------------
  * For every row:   s = x + residual, rounded to the type (no residual: s = x)
  *                  y = s * rsqrt(mean_c(s[c]^2) + eps) * weight[c]
- * s is kept as the next residual.  OGC_NORM_SAME: y in the type of x; OGC_NORM_MX4, OGC_NORM_MX8: y as a microscaled matrix, quantized from its
+ * s is kept as the next residual.  Squares of eight channels are added up in fp32, these sums in 64 bits (magnitudes from 2^62 on may make a sum infinite,
+ * and y zeros).  OGC_NORM_SAME: y in the type of x; OGC_NORM_MX4, OGC_NORM_MX8: y as a microscaled matrix, quantized from its
  * fp32 values as by ogc_mx_write. */
 typedef enum { OGC_NORM_SAME = 0, OGC_NORM_MX4 = 1, OGC_NORM_MX8 = 2 } ogc_norm_out;
 
@@ -81,12 +83,12 @@ ogc_status ogc_mx_read(const ogc_mx_rows* rows, const void* codes, const void* s
 
 /* ---- product ---------------------------------------------------------------------------------------------------------------------
  * y[i][j] = sum_c x[i][c] w[j][c] + bias[j],  x [m][k] and w [n][k] microscaled matrices.  Products and sums by the matrix instruction for
- * microscaled operands, fp32 results: of two OGC_MX4 matrices the products and the sums of one instruction are exact, of OGC_MX8 rows
- * the products of one instruction (64 channels) are added with some 2^-17 of the largest lost. */
+ * microscaled operands, fp32 sums: of two OGC_MX4 matrices the products and the sums of one instruction are exact, of OGC_MX8 rows
+ * the products of one instruction (64 channels) are added with some 2^-17 of the largest lost (measured: 7e-6 of a result of random rows). */
 typedef struct ogc_mx_product_desc {
     int32_t dtype;              /* of y */
     int32_t x_format, w_format; /* OGC_MX4 or OGC_MX8; OGC_MX4 */
-    int32_t m, n, k;            /* m >= 0; n, k > 0; k at most 2^20 */
+    int32_t m, n, k;            /* m >= 0; n, k > 0; at most 2^21, 2^26, 2^20, and (m / 256) * (n / 256), rounded up, 2^23 - 8 */
     int32_t has_bias;           /* 0 or 1 */
     int64_t y_stride;
 } ogc_mx_product_desc;

@@ -146,10 +146,12 @@ namespace {
 // 37.8 / 41.6, 8192 x 8192 x 1024 55 / 59, 4096 x 4096 x 2048 24.7 / 23.2, 2048 x 2048 x 8192 21.6 / 42.3, 8192 x 8192 x 8192 285 / 242; 8-bit rows 4096 x 4096 x 512
 // 15.0 / 15.4, 4096 x 4096 x 1024 21.4 / 20.5, 4096 x 8192 x 8192 216 / 189.
 enum { FEW_1, FEW_2, TILE_128, TILE_256 };
+constexpr int64_t MOST_SMALL = 0xfffff8, MOST_LARGE = 0x7ffff8;  // tiles of a launch of fewer than 2^32 threads, 256 and 512 a tile; multiples of eight
 int kernel_for(const ogc_mx_product_desc* d) {
     const auto count = [&](int64_t by) { return (d->n + by - 1) / by * ((d->m + by - 1) / by); };
     const int64_t blocks = count(32), small = count(128), large = count(256);
     if (blocks <= 1536) return blocks < 512 ? FEW_1 : FEW_2;
+    if (small > MOST_SMALL) return TILE_256;
     const double stages = mx_padded_channels(d->k) / 128, rest = small % 512 == 0 ? 0.0 : small % 512 <= 256 ? 0.6 : 1.0;
     const bool eight = d->x_format == OGC_MX8;
     const double of_small = ((double)(small / 512) + rest) * (3.0 + (eight ? 0.79 : 0.51) * stages);
@@ -190,7 +192,7 @@ ogc_status ogc_mx_product_validate(const ogc_mx_product_desc* d) {
         if (f != OGC_MX4 && f != OGC_MX8) return OGC_ERR_INVALID_ARG;
     if (d->has_bias != 0 && d->has_bias != 1) return OGC_ERR_INVALID_ARG;
     if (d->m < 0 || d->n <= 0 || d->k <= 0 || d->k > 1 << 20) return OGC_ERR_SHAPE;
-    if (d->m > 65535 * 32 || d->n > 32 * 0xffffff / 8) return OGC_ERR_SHAPE;  // blocks of a launch
+    if (d->m > 1 << 21 || d->n > 1 << 26 || ((int64_t)d->m + 255) / 256 * (((int64_t)d->n + 255) / 256) > MOST_LARGE) return OGC_ERR_SHAPE;
     if (d->w_format != OGC_MX4 || (d->dtype != OGC_F32 && d->dtype != OGC_BF16)) return OGC_ERR_UNSUPPORTED;
     if (d->y_stride < 0 || d->y_stride * (d->dtype == OGC_F32 ? 4 : 2) % 16 != 0) return OGC_ERR_ALIGNMENT;
     return OGC_OK;

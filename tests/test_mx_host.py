@@ -299,3 +299,12 @@ def test_reported_kernel_names_are_in_the_library():
                 for n in (64, 1000, 8192):
                     seen.add(b.ogc_mx_product_kernel_name(product(dtype=dtype, x_format=fmt, m=m, n=n, k=4096, y_stride=8192)))
     assert seen <= kernels
+
+
+@built
+def test_products_of_many_tiles():
+    """A launch has fewer than 2^32 threads: beyond 2^24 tiles of 128 x 128 the large ones, whatever k, and beyond 2^23 of those none."""
+    for k in (1, 256, 8192):
+        assert "2, 4, 4, 2>" in b.ogc_mx_product_kernel_name(product(m=1 << 20, n=1 << 18, k=k))
+    for m, n, status in ((1 << 21, 1 << 18, SHAPE), (1 << 21, (1 << 18) - 256, 0), ((1 << 21) + 1, 64, SHAPE), (64, (1 << 26) + 1, SHAPE), (64, 1 << 26, 0), (1 << 21, 1 << 26, SHAPE)):
+        assert b.ogc_mx_product_validate(product(m=m, n=n, y_stride=1 << 26)) == status, (m, n)
