@@ -22,6 +22,12 @@ def _types():
     return {torch.float32: binding.OGC_F32, torch.bfloat16: binding.OGC_BF16}
 
 
+def _type(dtype, what: str) -> int:
+    if dtype not in _types():
+        raise ValueError("%s of %s, not float32 or bfloat16" % (what, dtype))
+    return _types()[dtype]
+
+
 def _stream() -> int:
     import torch
 
@@ -38,8 +44,7 @@ def check_matrix(x, what: str, channels: Optional[int] = None) -> None:
     """ValueError unless x is rows as the calls take them: the kernels get an address and a stride, and believe them."""
     if x.dim() != 2 or (channels is not None and x.shape[1] != channels):
         raise ValueError("%s of shape %s, not [rows, %s]" % (what, list(x.shape), "channels" if channels is None else channels))
-    if x.dtype not in _types():
-        raise ValueError("%s of type %s, not float32 or bfloat16" % (what, x.dtype))
+    _type(x.dtype, what)
     if x.shape[1] > 1 and x.stride(1) != 1:
         raise ValueError("the channels of %s are %d elements apart, not next to each other" % (what, x.stride(1)))
     if x.shape[0] > 1 and (x.stride(0) < x.shape[1] or x.stride(0) * x.element_size() % 16):
@@ -82,9 +87,16 @@ class MxMatrix:
         binding.ogc_mx_write(rows, x.data_ptr(), m.codes.data_ptr(), m.scales.data_ptr(), _stream())
         return m
 
+    def check(self, what: str) -> None:
+        """ValueError unless the matrix is on the current GPU."""
+        if not on_this_gpu(self.codes):
+            raise ValueError("%s on %s, not on the current GPU" % (what, self.codes.device))
+
     def read(self, dtype):
+        kind = _type(dtype, "rows")
+        self.check("a matrix")
         y = _rows(self.rows, self.channels, dtype)
-        rows = binding.mx_rows(_types()[dtype], FORMATS[self.fmt], self.rows, self.channels, 0, _stride(y))
+        rows = binding.mx_rows(kind, FORMATS[self.fmt], self.rows, self.channels, 0, _stride(y))
         binding.ogc_mx_read(rows, self.codes.data_ptr(), self.scales.data_ptr(), y.data_ptr(), _stream())
         return y
 
@@ -93,6 +105,8 @@ def add_norm(x, residual, weight, eps: float = 1e-6, out: str = "same"):
     """(x + residual, its root-mean-square norm as rows or as a matrix); without a residual (None): (x, its norm)."""
     import torch
 
+    if out not in NORMS:
+        raise ValueError("a norm as %s, not same, mx4 or mx8" % (out,))
     check_matrix(x, "rows")
     if residual is not None:
         check_matrix(residual, "the residual", x.shape[1])
@@ -126,9 +140,12 @@ class Projection:
 
         if x.channels != self.weight.channels:
             raise ValueError("rows of %d channels for weights of %d" % (x.channels, self.weight.channels))
+        kind = _type(dtype, "a result")
+        x.check("rows")
+        self.weight.check("weights")
         n = self.weight.rows
         y = _rows(x.rows, n, dtype)
-        desc = binding.mx_product_desc(_types()[dtype], FORMATS[x.fmt], binding.OGC_MX4, x.rows, n, x.channels, int(self.bias is not None), _stride(y))
+        desc = binding.mx_product_desc(kind, FORMATS[x.fmt], binding.OGC_MX4, x.rows, n, x.channels, int(self.bias is not None), _stride(y))
         need = binding.ogc_mx_product_workspace_bytes(desc)
         space = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
         binding.ogc_mx_product_run(desc, x.codes.data_ptr(), x.scales.data_ptr(), self.weight.codes.data_ptr(), self.weight.scales.data_ptr(),
@@ -182,8 +199,7 @@ class TokenChoice:
     def __init__(self, rows: int, vocab: int, dtype, temperature=None, top_k=None, top_p=None, min_p=None):
         import torch
 
-        if dtype not in _types():
-            raise ValueError("logits of %s, not float32 or bfloat16" % (dtype,))
+        _type(dtype, "logits")
         for t, kind, what in ((temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"), (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p")):
             if t is not None and (t.dtype != kind or tuple(t.shape) != (rows,) or not t.is_contiguous() or not on_this_gpu(t)):
                 raise ValueError("%s of %s %s on %s, not %s [%d], contiguous, on the GPU" % (what, t.dtype, list(t.shape), t.device, kind, rows))
@@ -197,6 +213,8 @@ class TokenChoice:
 
         if tuple(logits.shape) != (self.rows, self.vocab) or logits.dtype != self.dtype or not on_this_gpu(logits) or (self.vocab > 1 and logits.stride(1) != 1):
             raise ValueError("logits of %s %s on %s, not %s [%d, %d], next to each other, on the GPU" % (logits.dtype, list(logits.shape), logits.device, self.dtype, self.rows, self.vocab))
+        if self.workspace.device != logits.device:
+            raise ValueError("logits on %s, the workspace on %s" % (logits.device, self.workspace.device))
         if uniform.dtype != torch.float32 or tuple(uniform.shape) != (self.rows,) or not uniform.is_contiguous() or uniform.device != logits.device:
             raise ValueError("uniform of %s %s on %s, not float32 [%d], contiguous, on %s" % (uniform.dtype, list(uniform.shape), uniform.device, self.rows, logits.device))
         tokens = torch.empty(self.rows, dtype=torch.int32, device="cuda")

@@ -31,6 +31,20 @@ def test_formats_and_limits_that_are_refused():
         dl.TokenChoice(2, 10, torch.float16)
 
 
+def test_matrices_elsewhere_and_types_that_are_refused():
+    m = dl.MxMatrix.__new__(dl.MxMatrix)
+    m.fmt, m.rows, m.channels, m.codes, m.scales = "mx8", 4, 256, torch.zeros(32 * 256, dtype=torch.uint8), torch.zeros(32 * 8, dtype=torch.uint8)
+    p = dl.Projection.__new__(dl.Projection)
+    p.weight, p.bias = m, None
+    for dtype in (torch.float32, torch.float16):  # (the first of a type that is right, but not on a GPU)
+        with pytest.raises(ValueError):
+            m.read(dtype)
+        with pytest.raises(ValueError):
+            p(m, dtype)
+    with pytest.raises(ValueError):
+        dl.add_norm(torch.zeros(4, 16), None, torch.ones(16), out="mx6")
+
+
 def layer(dtype, rows, seed=0, c=256, hidden=320, hq=4, hk=2, d=32, batch=2, tokens=64):
     g = torch.Generator().manual_seed(seed)
     w = lambda n, k: (torch.randn((n, k), generator=g) * k ** -0.5).cuda()  # noqa: E731
@@ -105,6 +119,19 @@ def test_a_layer_is_near_the_one_without_formats():
     want = mx.gated(gu[:, :320], gu[:, 320:]) @ w[3].T
     assert np.linalg.norm(f64(stream) - s2) <= 2 * 2.0 ** -4 * np.linalg.norm(s2)
     assert np.linalg.norm(f64(update) - want) <= 4 * 2.0 ** -4 * np.linalg.norm(want)
+
+
+@pytest.mark.gpu
+def test_prompts_without_tokens():
+    """A sequence without a prompt beside one with it, and none at all; then a token of each."""
+    a, b = layer("f32", "mx8", seed=5), layer("f32", "mx8", seed=5)
+    x, one = torch.randn((7, 256), generator=torch.Generator().manual_seed(3)).cuda(), torch.randn((2, 256), generator=torch.Generator().manual_seed(4)).cuda()
+    got, want = a.prefill(x, None, [0, 7]), b.prefill(x, None, [7, 0])
+    assert torch.equal(got[1], want[1]) and torch.isfinite(got[1]).all()
+    got, want = a.step(one, None), b.step(one.flip(0), None)
+    assert torch.equal(got[1], want[1].flip(0)) and torch.isfinite(got[1]).all()
+    assert a.prefill(x[:0], None, [0, 0])[1].shape == (0, 256)
+    assert torch.equal(a.step(one, None)[1][:1], got[1][:1])
 
 
 @pytest.mark.gpu
