@@ -67,21 +67,26 @@ struct Weights {
         const double x = logit;
         return x == largest ? 0.0 : (x - largest) * per;
     }
+    // p f + c, with c in scalar registers: written as an expression it costs a copy of c into vector registers each time, a third of all instructions
+    static __device__ __forceinline__ double next(double p, double f, double c) {
+        asm("v_fma_f64 %0, %0, %1, %2" : "+v"(p) : "v"(f), "s"(c));
+        return p;
+    }
     // 2^42 2^y, rounded, for y <= 0.  y = n + f, |f| <= 1/2: added to 3 * 2^51, y leaves n in the lower word; 2^f by the polynomial of degree 9 through its
     // values at the ten Chebyshev points, off by 2^-45.6; n goes into its exponent; and added to 2^52, what is left of the point is in the lower 52 bits.
     static __device__ __forceinline__ uint64_t of_log2(double y) {
         y = __builtin_fmax(y, -64.0);  // (no weight from -43 on)
         const double t = y + 0x1.8p52, f = y - (t - 0x1.8p52);
         double p = 0x1.b6571de2f2351p-24;
-        p = __builtin_fma(p, f, 0x1.63ef969a64d3cp-20);
-        p = __builtin_fma(p, f, 0x1.ffcb76789860fp-17);
-        p = __builtin_fma(p, f, 0x1.43088e257f341p-13);
-        p = __builtin_fma(p, f, 0x1.5d87fe908f88ap-10);
-        p = __builtin_fma(p, f, 0x1.3b2ab72b175eep-7);
-        p = __builtin_fma(p, f, 0x1.c6b08d7044119p-5);
-        p = __builtin_fma(p, f, 0x1.ebfbdff8149f2p-3);
-        p = __builtin_fma(p, f, 0x1.62e42fefa39f7p-1);
-        p = __builtin_fma(p, f, 0x1.000000000003dp+0);
+        p = next(p, f, 0x1.63ef969a64d3cp-20);
+        p = next(p, f, 0x1.ffcb76789860fp-17);
+        p = next(p, f, 0x1.43088e257f341p-13);
+        p = next(p, f, 0x1.5d87fe908f88ap-10);
+        p = next(p, f, 0x1.3b2ab72b175eep-7);
+        p = next(p, f, 0x1.c6b08d7044119p-5);
+        p = next(p, f, 0x1.ebfbdff8149f2p-3);
+        p = next(p, f, 0x1.62e42fefa39f7p-1);
+        p = next(p, f, 0x1.000000000003dp+0);
         const uint64_t bits = __builtin_bit_cast(uint64_t, p) + ((uint64_t)(((uint32_t)__builtin_bit_cast(uint64_t, t) + 42) << 20) << 32);
         return __builtin_bit_cast(uint64_t, __builtin_bit_cast(double, bits) + 0x1p52) & 0xfffffffffffffull;
     }
@@ -348,22 +353,29 @@ template <int DT, int RUNS> __global__ __launch_bounds__(SCAN_THREADS) void ogc_
     weights.largest = top;
     weights.per = l.per;
     const float high = place_of(top, l.fine);
-    const bool infinite = top == INFINITY;
+    const bool infinite = __builtin_amdgcn_readfirstlane(top == INFINITY);
     uint64_t sum = 0;
 #pragma unroll 1
-    for (int i = 0; i < RUNS; ++i) {  // (read once more, from the caches: with all of them unrolled the code takes longer to come than the exponentials)
-        Eight<DT> y;
-        y.load(row, first + i * SCAN_THREADS * 8 - off, a.vocab);
+    for (int i = 0; i < RUNS; ++i) {  // (one after the other through x[0]: with all of them unrolled the code takes longer to come than the exponentials)
+        uint64_t w[8];
+        if (infinite) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float v = y.get(e);
-            const uint64_t w = infinite ? Weights::of_infinite(v) : weights.of_part(v);
-            sum += w;
-            if (fill && w) {
-                const float d = high - place_of(v, l.fine);
-                if (d >= 0.0f && d < (float)FINE) atomicAdd((unsigned long long*)&bins[(int)d], (unsigned long long)w);
+            for (int e = 0; e < 8; ++e) w[e] = Weights::of_infinite(x[0].get(e));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = weights.of_part(x[0].get(e));
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += w[e];
+        if (fill) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float d = high - place_of(x[0].get(e), l.fine);
+                if (w[e] && d >= 0.0f && d < (float)FINE) atomicAdd((unsigned long long*)&bins[(int)d], (unsigned long long)w[e]);
             }
         }
+#pragma unroll
+        for (int j = 0; j + 1 < RUNS; ++j) x[j] = x[j + 1];
     }
     sum = wave_sum(sum);
     if (lane == 0) sums[wave] = sum;
@@ -582,17 +594,25 @@ template <int DT> SAMPLE_DEV void collect(const SampleArgs& a, Chosen& sh, const
             if (m[u] >= low && i >= 0 && i + 8 <= a.vocab) x[u].whole(row, i);
         }
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            if (!(m[u] >= low)) continue;
-            const int i = (i0 + u * THREADS) * 8 - off;
-            if (i < 0 || i + 8 > a.vocab) x[u].part(row, i, a.vocab);
+        for (int g = 0; g < AHEAD; g += 4) {  // (four chunks, a bit a token: put away together, since a wavefront goes on until its last lane has done so)
             uint32_t pass = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) pass |= x[u].get(e) >= low && x[u].get(e) <= high ? 1u << e : 0u;
+            for (int u = g + 3; u >= g; --u) {
+                uint32_t of_chunk = 0;
+                if (m[u] >= low) {
+                    const int i = (i0 + u * THREADS) * 8 - off;
+                    if (i < 0 || i + 8 > a.vocab) x[u].part(row, i, a.vocab);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) of_chunk |= x[u].get(e) >= low && x[u].get(e) <= high ? 1u << e : 0u;
+                }
+                pass = pass << 8 | of_chunk;
+            }
             if (!pass) continue;
             uint32_t to = atomicAdd(&sh.count, (uint32_t)__popc(pass));
-            for (; pass; pass &= pass - 1, ++to)
-                if (to < MOST) sh.tokens[to] = (uint32_t)(i + __ffs(pass) - 1);
+            for (; pass; pass &= pass - 1, ++to) {
+                const int bit = __ffs(pass) - 1;
+                if (to < MOST) sh.tokens[to] = (uint32_t)((i0 + (g + bit / 8) * THREADS) * 8 - off + bit % 8);
+            }
         }
     }
     __syncthreads();
