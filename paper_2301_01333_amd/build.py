@@ -228,10 +228,39 @@ def check_decoder_loops(verbose: bool = True) -> None:
             checked, len(prompts)), flush=True)
 
 
+def check_mx_loops(verbose: bool = True) -> None:
+    """The product's tiles count their direct loads as well: in their loop over the channels a wait for all but the newest in each of the two stages, and
+    none besides.  No kernel of the microscaled operators, and none that chooses tokens, may use scratch memory."""
+    import re
+
+    kernels = 0
+    for source, many in (("ogc_mx.hip", 12), ("ogc_norm.hip", 37), ("ogc_mx_product.hip", 16), ("ogc_sample.hip", 8)):
+        text = _device_assembly(source)
+        found = re.findall(r"\.name:\s+(\w*ogc_\w*kernel\w+)\s*\n\s+\.private_segment_fixed_size:\s+(\d+)", text)
+        if len(found) != many or any(int(scratch) for _, scratch in found):
+            raise RuntimeError("%s: %d kernels, not %d (name, bytes of scratch memory per lane): %s" % (source, len(found), many, found))
+        kernels += many
+        if source != "ogc_mx_product.hip":
+            continue
+        tiles = re.findall(r"^(\w*ogc_mx_tile_kernelI\w*):[^\n]*\n(.*?)\n\.Lfunc_end", text, re.S | re.M)
+        for name, code in tiles:
+            lines = [l.split(";")[0] for l in code.splitlines()]
+            bodies = [lines[a:b] for a, b in _loops(lines) if any("v_mfma" in l for l in lines[a:b]) and any("global_load_lds" in l for l in lines[a:b])]
+            body = min(bodies, key=len) if bodies else []
+            waits = [l.split()[1] for l in body if "s_waitcnt" in l and "vmcnt" in l]
+            if len(waits) != 2 or "vmcnt(0)" in waits:
+                raise RuntimeError("%s: its loop over the channels waits for %s" % (name, waits))
+        if len(tiles) != 8:
+            raise RuntimeError("%d kernels of tiles found in the assembly, not 8" % len(tiles))
+    if verbose:
+        print("microscaled operators' and token choice's kernels checked: %d (no scratch memory; no waits but the counted ones in the product's loops)" % kernels, flush=True)
+
+
 if __name__ == "__main__":
     print(build_library())
     check_stream_kernel_registers()
     check_split_attention_loops()
     check_int8_attention_loops()
     check_decoder_loops()
+    check_mx_loops()
     sys.exit(0)

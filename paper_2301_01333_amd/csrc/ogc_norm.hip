@@ -157,9 +157,17 @@ template <int DT, int OUT, int ROWS> void launch(const NormArgs& a, hipStream_t 
             return;
         }
     }
-    if (runs <= 4) hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, ROWS, 4>), g, t, 0, st, a);
-    else if (DT == OGC_BF16 && runs <= 8) hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, ROWS, 8>), g, t, 0, st, a);
-    else hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, ROWS, 0>), g, t, 0, st, a);
+    if (runs <= 4) {
+        hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, ROWS, 4>), g, t, 0, st, a);
+        return;
+    }
+    if constexpr (DT == OGC_BF16) {  // (in fp32 they would not fit the registers)
+        if (runs <= 8) {
+            hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, ROWS, 8>), g, t, 0, st, a);
+            return;
+        }
+    }
+    hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, ROWS, 0>), g, t, 0, st, a);
 }
 template <int DT> void launch(int out, const NormArgs& a, hipStream_t s) {
     const bool few = a.rows < 8 * 256;  // (eight rows each would leave compute units without work: 64 x 8192 in bf16 to 8 bits 5.7 us, eight rows each 12.5)
