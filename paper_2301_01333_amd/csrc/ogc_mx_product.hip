@@ -2,6 +2,7 @@
 #include "ogc_lds_limit.h"
 #include "ogc_mx_rows.h"
 
+#include <algorithm>
 #include <type_traits>
 
 typedef int v4i __attribute__((ext_vector_type(4)));
@@ -20,6 +21,7 @@ struct ProductArgs {
     int m, n, padded;
     int steps;  // of 256 channels
     int tiles_n, tiles_m;
+    int fewer_weights;
 };
 
 // One operand of one instruction: 64 channels of 32 rows, which lie in memory as its lanes take them.
@@ -65,98 +67,123 @@ template <int DT> MX_DEV void put4(const ProductArgs& a, int row, int n0, v4f v)
 
 constexpr int FEW_WAVES = 4;
 
-// A workgroup has NB blocks of 32 weights and 32 rows; its wavefronts take the channels in turn, 256 at a time, straight from memory into registers
-// (nothing that one of them reads is read by another of them), and add up in LDS.  Bound by memory: 32 x 32000 x 4096 with 8-bit rows 12.6 us, 5.7 TB/s; a
-// call that does not fill the chip by the latency of its loads, which are all on their way at once (32 x 8192 x 4096 4.8 us, with loads as the compiler
-// would have them 6.1).
-template <int DT, int XF, int NB> __global__ __launch_bounds__(64 * FEW_WAVES) void ogc_mx_few_kernel(ProductArgs a) {
+// A workgroup has NB blocks of 32 weights and MB blocks of 32 rows; its wavefronts take the channels in turn, 256 at a time, straight from memory into registers
+// (nothing that one of them reads is read by another of them), and add up in LDS.  Bound by memory where rows are few: 32 x 32000 x 4096 with 8-bit rows
+// 12.9 us, 5.7 TB/s; a call that does not fill the chip by the latency of its loads, which are all on their way at once (32 x 8192 x 4096 4.4 us, with loads as
+// the compiler would have them 6.1); in between by what a compute unit's load path brings in, some 40 bytes a clock (256 x 8192 x 4096 12.0 us).
+template <int DT, int XF, int NB, int MB> __global__ __launch_bounds__(64 * FEW_WAVES) void ogc_mx_few_kernel(ProductArgs a) {
     constexpr int PITCH = 36;  // floats of a row's 32 sums: the 16-byte pieces of eight rows are on distinct banks
     __shared__ __attribute__((aligned(16))) float sums[FEW_WAVES][32 * PITCH];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n0 = blockIdx.x * NB, m0 = blockIdx.y;  // in blocks of 32
-    const int last = (a.n + 31) / 32 - 1;
-    const uint8_t *w[NB], *ws[NB];
+    // Workgroup i runs on XCD i % 8: an XCD has neighbouring weights, and all rows that meet them one after the other (256 x 32000 x 4096 in blocks of 64 x 64:
+    // 39.8 us, 47 with all weights for the first rows first); the other way round where the weights have fewer bytes than the rows.
+    const int tiles = a.tiles_n * a.tiles_m, each = (tiles + 7) / 8, tile = blockIdx.x % 8 * each + blockIdx.x / 8;
+    if (blockIdx.x / 8 >= (uint32_t)each || tile >= tiles) return;
+    const int tn = a.fewer_weights ? tile % a.tiles_n : tile / a.tiles_m, tm = a.fewer_weights ? tile / a.tiles_n : tile % a.tiles_m;
+    const int n0 = tn * NB, m0 = tm * MB;  // in blocks of 32
+    const int last = (a.n + 31) / 32 - 1, last_row = (a.m + 31) / 32 - 1;
+    const uint8_t *w[NB], *ws[NB], *x[MB], *xs[MB];
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
         const int b = min(n0 + i, last);
         w[i] = a.w + b * mx_codes_of_32(OGC_MX4, a.padded) + lane * 16;
         ws[i] = a.ws + (int64_t)b * a.padded + lane * 4;
     }
-    const uint8_t* const x = a.x + m0 * mx_codes_of_32(XF, a.padded) + lane * 16;
-    const uint8_t* const xs = a.xs + (int64_t)m0 * a.padded + lane * 4;
-    v16f c[NB];
+#pragma unroll
+    for (int j = 0; j < MB; ++j) {
+        const int b = min(m0 + j, last_row);
+        x[j] = a.x + b * mx_codes_of_32(XF, a.padded) + lane * 16;
+        xs[j] = a.xs + (int64_t)b * a.padded + lane * 4;
+    }
+    v16f c[NB][MB];
 #pragma unroll
     for (int i = 0; i < NB; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) c[i][e] = 0.0f;
+        for (int j = 0; j < MB; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) c[i][j][e] = 0.0f;
     for (int s = wave; s < a.steps; s += FEW_WAVES) {
         Operand<OGC_MX4> p[NB][4];
-        Operand<XF> q[4];
-        uint32_t u[NB];
+        Operand<XF> q[MB][4];
+        uint32_t u[NB], v[MB];
 #pragma unroll
         for (int i = 0; i < NB; ++i) u[i] = *(const uint32_t*)(ws[i] + (int64_t)s * 256);
-        const uint32_t v = *(const uint32_t*)(xs + (int64_t)s * 256);
+#pragma unroll
+        for (int j = 0; j < MB; ++j) v[j] = *(const uint32_t*)(xs[j] + (int64_t)s * 256);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
 #pragma unroll
             for (int i = 0; i < NB; ++i) p[i][t].load(w[i] + ((int64_t)s * 4 + t) * Operand<OGC_MX4>::BYTES);
-            q[t].load(x + ((int64_t)s * 4 + t) * Operand<XF>::BYTES);
+#pragma unroll
+            for (int j = 0; j < MB; ++j) q[j][t].load(x[j] + ((int64_t)s * 4 + t) * Operand<XF>::BYTES);
         }
         __builtin_amdgcn_sched_barrier(0);  // (all of them on their way before the first is waited for)
 #pragma unroll
-        for (int i = 0; i < NB; ++i) {
-            c[i] = product<XF, 0>(p[i][0], q[0], c[i], u[i], v);
-            c[i] = product<XF, 1>(p[i][1], q[1], c[i], u[i], v);
-            c[i] = product<XF, 2>(p[i][2], q[2], c[i], u[i], v);
-            c[i] = product<XF, 3>(p[i][3], q[3], c[i], u[i], v);
-        }
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int j = 0; j < MB; ++j) {
+                c[i][j] = product<XF, 0>(p[i][0], q[j][0], c[i][j], u[i], v[j]);
+                c[i][j] = product<XF, 1>(p[i][1], q[j][1], c[i][j], u[i], v[j]);
+                c[i][j] = product<XF, 2>(p[i][2], q[j][2], c[i][j], u[i], v[j]);
+                c[i][j] = product<XF, 3>(p[i][3], q[j][3], c[i][j], u[i], v[j]);
+            }
     }
     const int row = threadIdx.x / 8, at = threadIdx.x % 8 * 4;
 #pragma unroll
-    for (int i = 0; i < NB; ++i) {
-        if (i > 0) __syncthreads();
-        // lane l has the weights 8 q + 4 (l / 32) .. of row l % 32 in its registers 4 q ..
+    for (int i = 0; i < NB; ++i)
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            *(v4f*)(&sums[wave][lane % 32 * PITCH + q * 8 + lane / 32 * 4]) = (v4f){c[i][4 * q], c[i][4 * q + 1], c[i][4 * q + 2], c[i][4 * q + 3]};
-        __syncthreads();
-        const int n = (n0 + i) * 32 + at;
-        v4f v = *(const v4f*)(&sums[0][row * PITCH + at]);
+        for (int j = 0; j < MB; ++j) {
+            if (i + j > 0) __syncthreads();
+            // lane l has the weights 8 q + 4 (l / 32) .. of row l % 32 in its registers 4 q ..
 #pragma unroll
-        for (int k = 1; k < FEW_WAVES; ++k) v += *(const v4f*)(&sums[k][row * PITCH + at]);
-        if (a.bias) {
+            for (int q = 0; q < 4; ++q)
+                *(v4f*)(&sums[wave][lane % 32 * PITCH + q * 8 + lane / 32 * 4]) = (v4f){c[i][j][4 * q], c[i][j][4 * q + 1], c[i][j][4 * q + 2], c[i][j][4 * q + 3]};
+            __syncthreads();
+            const int n = (n0 + i) * 32 + at;
+            v4f v = *(const v4f*)(&sums[0][row * PITCH + at]);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] += n + k < a.n ? a.bias[n + k] : 0.0f;
+            for (int k = 1; k < FEW_WAVES; ++k) v += *(const v4f*)(&sums[k][row * PITCH + at]);
+            if (a.bias) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] += n + k < a.n ? a.bias[n + k] : 0.0f;
+            }
+            put4<DT>(a, (m0 + j) * 32 + row, n, v);
         }
-        put4<DT>(a, m0 * 32 + row, n, v);
-    }
 }
 
 #include "ogc_mx_tile.h"
 
 namespace {
 
-// Which kernel a call takes: the same for its launch and its name.  Few blocks of 32 x 32: wavefronts that share the channels, one block each where
-// workgroups of two would not give every compute unit two of them (m x n x k, 8-bit rows, one block / two, us: 32 x 8192 x 4096 4.8 / 5.6, 64 x 8192 x 4096
-// 6.8 / 5.9, 128 x 8192 x 4096 10.4 / 8.4).  More: tiles in LDS, from 1536 blocks on (two blocks / tiles of 128 x 128: 128 x 8192 x 4096 8.4 / 13.6, 256 x 8192 x
-// 4096 15 / 14.4, 4096 x 4096 x 512 18.8 / 12.8).
+// Which kernel a call takes, the same for its launch and its name: the one that takes the least time by costs that are fitted to all five of them at 190 sizes
+// (m 16 .. 8192, n 90 .. 32000, k 64 .. 16000; the choice is 0.6 % above the fastest in the mean, 17 % at most).  us, of wavefronts that share the channels in
+// blocks of 32 x 32 / 64 x 32 / 64 x 64, and of tiles of 128 x 128 / 256 x 256, m x n x k with 8-bit rows: 32 x 8192 x 4096 4.4 / 4.8 / 7.0 / 14.7 / 39; 128 x 8192 x 4096
+// 9.8 / 8.0 / 7.7 / 13.5 / 39; 256 x 8192 x 4096 16.6 / 13.0 / 12.0 / 13.9 / 37; 512 x 8192 x 4096 30 / 23 / 21 / 17.9 / 39; 1024 x 14336 x 4096 123 / 91 / 74 / 56 / 48.
+// A wavefront's share of 256 channels takes its own time, or its part of what all workgroups have to pull in; the ones beyond 512 take turns, ends included.
 // Tiles of 256 x 256 have a compute unit to themselves, so that 256 of them take as long as one, and no product hides their first loads and last stores;
-// two of 128 x 128 share a compute unit, but pull twice the bytes through LDS.  A round of 512 small tiles takes 3 + 0.51 us for 128 channels (half of them 0.6
-// of that), one of 256 large ones 7 + 0.83, with 8-bit rows 3 + 0.79 and 7 + 1.36, fitted to small / large, us: 4 bits 4096 x 4096 x 512 12.8 / 12.9, 8192 x 8192 x 512
-// 37.8 / 41.6, 8192 x 8192 x 1024 55 / 59, 4096 x 4096 x 2048 24.7 / 23.2, 2048 x 2048 x 8192 21.6 / 42.3, 8192 x 8192 x 8192 285 / 242; 8-bit rows 4096 x 4096 x 512
-// 15.0 / 15.4, 4096 x 4096 x 1024 21.4 / 20.5, 4096 x 8192 x 8192 216 / 189.
-enum { FEW_1, FEW_2, TILE_128, TILE_256 };
+// two of 128 x 128 share a compute unit, but pull twice the bytes through LDS (small / large, us: 4 bits 8192 x 8192 x 512 37.8 / 41.6, 4096 x 4096 x 2048
+// 24.7 / 23.2, 8192 x 8192 x 8192 285 / 242; 8-bit rows 4096 x 4096 x 512 15.0 / 15.4, 4096 x 8192 x 8192 216 / 189).
+enum { FEW_1, FEW_2, FEW_4, TILE_128, TILE_256 };
 constexpr int64_t MOST_SMALL = 0xfffff8, MOST_LARGE = 0x7ffff8;  // tiles of a launch of fewer than 2^32 threads, 256 and 512 a tile; multiples of eight
 int kernel_for(const ogc_mx_product_desc* d) {
-    const auto count = [&](int64_t by) { return (d->n + by - 1) / by * ((d->m + by - 1) / by); };
-    const int64_t blocks = count(32), small = count(128), large = count(256);
-    if (blocks <= 1536) return blocks < 512 ? FEW_1 : FEW_2;
+    const auto count = [&](int64_t by_n, int64_t by_m) { return (d->n + by_n - 1) / by_n * ((d->m + by_m - 1) / by_m); };
+    const int64_t small = count(128, 128);
     if (small > MOST_SMALL) return TILE_256;
-    const double stages = mx_padded_channels(d->k) / 128, rest = small % 512 == 0 ? 0.0 : small % 512 <= 256 ? 0.6 : 1.0;
     const bool eight = d->x_format == OGC_MX8;
-    const double of_small = ((double)(small / 512) + rest) * (3.0 + (eight ? 0.79 : 0.51) * stages);
-    const double of_large = (double)((large + 255) / 256) * (7.0 + (eight ? 1.36 : 0.83) * stages);
-    return of_small < of_large ? TILE_128 : TILE_256;
+    const double stages = mx_padded_channels(d->k) / 128, share = stages / (2 * FEW_WAVES);
+    const auto few = [&](int64_t groups, double start, double own, double part, double turn) {
+        return start + share * std::max(own, part * (double)groups) + turn * (double)std::max<int64_t>(0, groups - 512);
+    };
+    const int64_t rest = small % 512;
+    const double of_rest = rest == 0 ? 0.0 : eight ? 4.3 + 0.96 * stages * (rest <= 128 ? 0.34 : rest <= 256 ? 0.43 : 1.0)
+                                                   : 4.7 + 0.68 * stages * (rest <= 128 ? 0.29 : rest <= 256 ? 0.40 : 1.0);
+    const double cost[5] = {eight ? few(count(32, 32), 2.6, 0.36, 0.0018, 0.00043) : few(count(32, 32), 2.7, 0.24, 0.0013, 0.00044),
+                            eight ? few(count(64, 32), 3.4, 0.45, 0.0025, 0.0010) : few(count(64, 32), 3.5, 0.30, 0.0017, 0.0012),
+                            eight ? few(count(64, 64), 4.8, 0.79, 0.0041, 0.0032) : few(count(64, 64), 5.2, 0.43, 0.0026, 0.0023),
+                            (double)(small / 512) * (3.0 + (eight ? 0.79 : 0.51) * stages) + of_rest,
+                            (double)((count(256, 256) + 255) / 256) * (7.0 + (eight ? 1.36 : 0.83) * stages)};
+    const int first = count(32, 32) > MOST_SMALL ? TILE_128 : FEW_1;
+    return (int)(std::min_element(cost + first, cost + 5) - cost);
 }
 
 template <int DT, int XF, int WN, int WM, int NB, int MB> bool launch_tiles(ProductArgs a, hipStream_t s) {
@@ -172,12 +199,17 @@ template <int DT, int XF, int WN, int WM, int NB, int MB> bool launch_tiles(Prod
     hipLaunchKernelGGL((ogc_mx_tile_kernel<DT, XF, WN, WM, NB, MB>), dim3(grid), dim3(64 * T::WAVES), T::LDS, s, a);
     return true;
 }
+template <int DT, int XF, int NB, int MB> void launch_few(ProductArgs a, hipStream_t s) {
+    a.tiles_n = (a.n + NB * 32 - 1) / (NB * 32);
+    a.tiles_m = (a.m + MB * 32 - 1) / (MB * 32);
+    hipLaunchKernelGGL((ogc_mx_few_kernel<DT, XF, NB, MB>), dim3((a.tiles_n * a.tiles_m + 7) / 8 * 8), dim3(64 * FEW_WAVES), 0, s, a);
+}
 template <int DT, int XF> bool launch(int which, const ProductArgs& a, hipStream_t s) {
     if (which == TILE_256) return launch_tiles<DT, XF, 2, 4, 4, 2>(a, s);
     if (which == TILE_128) return launch_tiles<DT, XF, 2, 2, 2, 2>(a, s);
-    const unsigned m = (unsigned)((a.m + 31) / 32);
-    if (which == FEW_1) hipLaunchKernelGGL((ogc_mx_few_kernel<DT, XF, 1>), dim3((a.n + 31) / 32, m), dim3(64 * FEW_WAVES), 0, s, a);
-    else hipLaunchKernelGGL((ogc_mx_few_kernel<DT, XF, 2>), dim3((a.n + 63) / 64, m), dim3(64 * FEW_WAVES), 0, s, a);
+    if (which == FEW_1) launch_few<DT, XF, 1, 1>(a, s);
+    else if (which == FEW_2) launch_few<DT, XF, 2, 1>(a, s);
+    else launch_few<DT, XF, 2, 2>(a, s);
     return true;
 }
 
@@ -208,9 +240,10 @@ ogc_status ogc_mx_product_workspace_bytes(const ogc_mx_product_desc* d, size_t* 
 
 const char* ogc_mx_product_kernel_name(const ogc_mx_product_desc* d) {
     if (ogc_mx_product_validate(d) != OGC_OK) return nullptr;
-    static const char* const names[4][2][2] = {
-        {{"ogc_mx_few_kernel<0, 0, 1>", "ogc_mx_few_kernel<0, 1, 1>"}, {"ogc_mx_few_kernel<1, 0, 1>", "ogc_mx_few_kernel<1, 1, 1>"}},
-        {{"ogc_mx_few_kernel<0, 0, 2>", "ogc_mx_few_kernel<0, 1, 2>"}, {"ogc_mx_few_kernel<1, 0, 2>", "ogc_mx_few_kernel<1, 1, 2>"}},
+    static const char* const names[5][2][2] = {
+        {{"ogc_mx_few_kernel<0, 0, 1, 1>", "ogc_mx_few_kernel<0, 1, 1, 1>"}, {"ogc_mx_few_kernel<1, 0, 1, 1>", "ogc_mx_few_kernel<1, 1, 1, 1>"}},
+        {{"ogc_mx_few_kernel<0, 0, 2, 1>", "ogc_mx_few_kernel<0, 1, 2, 1>"}, {"ogc_mx_few_kernel<1, 0, 2, 1>", "ogc_mx_few_kernel<1, 1, 2, 1>"}},
+        {{"ogc_mx_few_kernel<0, 0, 2, 2>", "ogc_mx_few_kernel<0, 1, 2, 2>"}, {"ogc_mx_few_kernel<1, 0, 2, 2>", "ogc_mx_few_kernel<1, 1, 2, 2>"}},
         {{"ogc_mx_tile_kernel<0, 0, 2, 2, 2, 2>", "ogc_mx_tile_kernel<0, 1, 2, 2, 2, 2>"}, {"ogc_mx_tile_kernel<1, 0, 2, 2, 2, 2>", "ogc_mx_tile_kernel<1, 1, 2, 2, 2, 2>"}},
         {{"ogc_mx_tile_kernel<0, 0, 2, 4, 4, 2>", "ogc_mx_tile_kernel<0, 1, 2, 4, 4, 2>"}, {"ogc_mx_tile_kernel<1, 0, 2, 4, 4, 2>", "ogc_mx_tile_kernel<1, 1, 2, 4, 4, 2>"}}};
     return names[kernel_for(d)][d->dtype][d->x_format];
@@ -240,6 +273,7 @@ ogc_status ogc_mx_product_run(const ogc_mx_product_desc* d, const void* x, const
     const hipStream_t s = (hipStream_t)stream;
     a.tiles_n = a.tiles_m = 0;
     const bool eight = d->x_format == OGC_MX8;
+    a.fewer_weights = d->n < (eight ? 2 : 1) * (int64_t)d->m;
     const int which = kernel_for(d);
     const bool sent = d->dtype == OGC_F32 ? (eight ? launch<OGC_F32, OGC_MX8>(which, a, s) : launch<OGC_F32, OGC_MX4>(which, a, s))
                                           : (eight ? launch<OGC_BF16, OGC_MX8>(which, a, s) : launch<OGC_BF16, OGC_MX4>(which, a, s));

@@ -385,9 +385,11 @@ def test_products_of_whole_numbers_are_exact(xf, m, n, k):
 @pytest.mark.parametrize("xf", ["mx4", "mx8"])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("m,n,k,kernel", [
-    (100, 90, 700, "few_kernel<%d, %d, 1>"), (33, 8200, 300, "few_kernel<%d, %d, 2>"), (1030, 1290, 300, "few_kernel<%d, %d, 2>"),
-    (1300, 1250, 200, "tile_kernel<%d, %d, 2, 2, 2, 2>"), (1301, 1251, 900, "tile_kernel<%d, %d, 2, 2, 2, 2>"), (129, 14000, 260, "tile_kernel<%d, %d, 2, 2, 2, 2>"),
-    (3000, 4000, 100, "tile_kernel<%d, %d, 2, 2, 2, 2>"), (3900, 3900, 700, "tile_kernel<%d, %d, 2, 4, 4, 2>"), (3841, 4001, 1300, "tile_kernel<%d, %d, 2, 4, 4, 2>")])
+    (100, 90, 700, "few_kernel<%d, %d, 1, 1>"), (33, 8200, 300, "few_kernel<%d, %d, 1, 1>"), (33, 14300, 2100, "few_kernel<%d, %d, 2, 1>"), (300, 2000, 4000, "few_kernel<%d, %d, 2, 1>"),
+    (255, 8000, 4100, "few_kernel<%d, %d, 2, 2>"), (317, 11383, 1700, "few_kernel<%d, %d, 2, 2>"),
+    (401, 12765, 200, "tile_kernel<%d, %d, 2, 2, 2, 2>"), (354, 9393, 300, "tile_kernel<%d, %d, 2, 2, 2, 2>"), (226, 12461, 700, "tile_kernel<%d, %d, 2, 2, 2, 2>"),
+    (162, 15797, 900, "tile_kernel<%d, %d, 2, 2, 2, 2>"), (788, 14543, 200, "tile_kernel<%d, %d, 2, 4, 4, 2>"), (1038, 11039, 300, "tile_kernel<%d, %d, 2, 4, 4, 2>"),
+    (3900, 3900, 1700, "tile_kernel<%d, %d, 2, 4, 4, 2>"), (3841, 4001, 1300, "tile_kernel<%d, %d, 2, 4, 4, 2>")])
 def test_product_by_kernel(xf, dtype, m, n, k, kernel):
     """Every kernel, with one stage of channels and with many, whole tiles and ragged ones."""
     _, _, name = run_product(xf, dtype, m, n, k, bias=k % 3 == 0)
