@@ -704,21 +704,24 @@ template <int EACH> SAMPLE_DEV int kept_of(Chosen& sh, int n, const Weights& wei
 template <int DT> SAMPLE_DEV bool by_top_k(const SampleArgs& a, Chosen& sh, const uint8_t* row, const Limits& l, const Weights& weights, float high, float u, int r, Result& found) {
     const float* const tops = a.tops + (int64_t)r * a.chunks;
     const auto away = [&](float x) { return high - place_of(x, l.fine); };
-    // ---- the bin of the k-th of 1024 largest logits, a thread each
+    // ---- the bin of the k-th of 2048 largest logits, two a thread (of 1024 the thousandth would have some four thousand tokens before it)
     sh.counts[threadIdx.x] = 0;
     if (threadIdx.x == 0) sh.count = 0, sh.low = 0xffffffffu, sh.found = FINE;
-    float m = -INFINITY;
+    float m[2] = {-INFINITY, -INFINITY}, d[2];
 #pragma unroll 1
     for (int i = threadIdx.x; i < a.chunks; i += 8 * THREADS) {
         float t[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u) t[u] = tops[min(i + u * THREADS, a.chunks - 1)];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) m = i + u * THREADS < a.chunks ? fmaxf(m, t[u]) : m;
+        for (int u = 0; u < 8; ++u) m[u % 2] = i + u * THREADS < a.chunks ? fmaxf(m[u % 2], t[u]) : m[u % 2];
     }
-    const float d = m == -INFINITY ? (float)FINE : away(m);
     __syncthreads();
-    if (d < (float)FINE) atomicAdd(&sh.counts[(int)d], 1u);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        d[h] = m[h] == -INFINITY ? (float)FINE : away(m[h]);
+        if (d[h] < (float)FINE) atomicAdd(&sh.counts[(int)d[h]], 1u);
+    }
     __syncthreads();
     uint64_t all;
     const uint64_t c = sh.counts[threadIdx.x], s = sum_before(c, sh.part, all), k = (uint64_t)l.k;
@@ -726,7 +729,9 @@ template <int DT> SAMPLE_DEV bool by_top_k(const SampleArgs& a, Chosen& sh, cons
     __syncthreads();
     // the smallest of those up to that bin: k tokens at least are as large.  (Fewer than k with a weight: all that have one.)
     const bool enough = sh.found < FINE;
-    if (enough && d <= (float)sh.found) atomicMin(&sh.low, key_of(m));
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        if (enough && d[h] <= (float)sh.found) atomicMin(&sh.low, key_of(m[h]));
     __syncthreads();
     const uint32_t low = enough ? sh.low : first_at(high - (float)(FINE - 1), l.fine);
     collect<DT>(a, sh, row, logit_of(low), INFINITY);
