@@ -14,8 +14,9 @@
  * ones, with log-probability 0.  top_k <= 0, top_p >= 1 or NaN, min_p <= 0 or
  * NaN: no such limit.  A uniform below 0 or NaN counts as 0, one from 1 on takes the last kept token.  Logits of +infinity share the choice
  * among them.  A row without any token: -1, with log-probability -infinity.
- * Weights are computed in 64 bits, rounded to multiples of 2^-42 (a token of less than 2^-43 of the largest one's weight has none) and added up exactly, so
- * that no order of additions decides at a limit, and a call gives the same tokens every time.
+ * Weights are computed in 64 bits and rounded to multiples of 2^-42 of the largest one of the row, or of a part of it (a token of less than 2^-43 of that has none).
+ * They are added up as whole numbers, or in a fixed order, so that a call gives the same tokens every time; a decision that is closer than
+ * vocab * 2^-42 of the sum it is compared with may fall either way.
  *
  * Calls are asynchronous on `stream` (a hipStream_t, NULL = the default stream) and may be captured into a graph; the library allocates nothing and keeps
  * nothing between calls.  Errors are return codes as in ogc_mx.h, found before any launch.  Calls without rows do nothing.
@@ -36,9 +37,9 @@ typedef struct ogc_sample_desc {
 } ogc_sample_desc;
 
 ogc_status ogc_sample_validate(const ogc_sample_desc* desc);
-/* Bytes that a call needs at `workspace` (0: none). */
+/* Bytes that a call needs at `workspace` (0: none): half a byte for each logit, and 8 KiB for every 2048 to 8192 of a row. */
 ogc_status ogc_sample_workspace_bytes(const ogc_sample_desc* desc, size_t* bytes);
-/* logits: 16-byte aligned or not (aligned rows are read faster).  temperature, top_p, min_p, uniform: fp32 [rows], top_k: int32 [rows]; each but `uniform` may
+/* logits: of any alignment of their type, and of any stride: rows are read 16 bytes at a time either way.  temperature, top_p, min_p, uniform: fp32 [rows], top_k: int32 [rows]; each but `uniform` may
  * be NULL (temperature 1, no limit).  tokens: int32 [rows]; log_probabilities: fp32 [rows], or NULL.  workspace: 16-byte aligned, contents do
  * not matter; calls that may run at the same time need different ones. */
 ogc_status ogc_sample_run(const ogc_sample_desc* desc, const void* logits, const float* temperature, const int32_t* top_k,

