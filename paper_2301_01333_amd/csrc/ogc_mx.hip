@@ -16,7 +16,6 @@ struct RowsArgs {
     uint8_t* scales;
     long long stride;  // bytes
     int rows, channels, padded, blocks;  // blocks: of 256 channels
-    int even;          // gate: the second halves of the rows are 16-byte aligned, too
 };
 
 // a * b / (1 + exp(-a)).  exp(-|a|) neither overflows nor loses what the product of |a| and log2(e) is rounded by (from |a| = 104 on it is 0 in fp32, and from
@@ -42,14 +41,7 @@ template <int DT, int FORMAT, int GATE> __global__ __launch_bounds__(256) void o
     for (int s = 0; s < 4; ++s) {
         const int c = c0 + s * 64, there = on ? a.channels - c : 0;
         x[s].load(p + (int64_t)c * E, there);
-        if constexpr (GATE) {
-            const uint8_t* const q = p + ((int64_t)a.channels + c) * E;
-            if (a.even) y[s].load(q, there);
-            else {
-                y[s].clear();
-                y[s].one_by_one(q, there);
-            }
-        }
+        if constexpr (GATE) y[s].load(p + ((int64_t)a.channels + c) * E, there);  // (of any alignment of a channel)
     }
     uint32_t scales = 0;
     mx_v2u code[4];
@@ -133,7 +125,6 @@ template <bool WRITE> ogc_status move(const ogc_mx_rows* d, const void* x, const
     a.channels = d->channels;
     a.padded = mx_padded_channels(d->channels);
     a.blocks = a.padded / MX_BLOCK;
-    a.even = (int64_t)d->channels * e % 16 == 0;
     const dim3 grid((unsigned)(mx_padded_rows(d->rows) / MX_ROWS * a.blocks)), threads(256);  // (checked: below 2^24)
     const hipStream_t s = (hipStream_t)stream;
     const int which = (d->dtype == OGC_F32 ? 4 : 0) + (d->format == OGC_MX8 ? 2 : 0) + (d->gate == OGC_GATE_SILU ? 1 : 0);

@@ -16,6 +16,7 @@ typedef float mx_v2f __attribute__((ext_vector_type(2)));
 typedef float mx_v4f __attribute__((ext_vector_type(4)));
 typedef uint32_t mx_v2u __attribute__((ext_vector_type(2)));
 typedef uint32_t mx_v4u __attribute__((ext_vector_type(4)));
+typedef uint32_t mx_v4u_anywhere __attribute__((ext_vector_type(4), aligned(2)));  // (loaded by the same instruction as an aligned one)
 typedef __bf16 mx_v2bf __attribute__((ext_vector_type(2)));
 typedef short mx_v2s __attribute__((ext_vector_type(2)));
 
@@ -26,23 +27,20 @@ template <int DT> struct MxEight {
 #pragma unroll
         for (int i = 0; i < (DT == OGC_F32 ? 2 : 1); ++i) raw[i] = (mx_v4u){0, 0, 0, 0};
     }
-    // the first `there` of the eight channels at p (16-byte aligned if all are there), zeros for the others; nothing else is touched
+    // the first `there` of the eight channels at p, zeros for the others; nothing else is touched
     __device__ __forceinline__ void load(const uint8_t* p, int there) {
         if (there >= 8) {
-            raw[0] = *(const mx_v4u*)p;
-            if constexpr (DT == OGC_F32) raw[1] = *(const mx_v4u*)(p + 16);
+            raw[0] = *(const mx_v4u_anywhere*)p;
+            if constexpr (DT == OGC_F32) raw[1] = *(const mx_v4u_anywhere*)(p + 16);
         } else {
             clear();
-            one_by_one(p, there);
-        }
-    }
-    __device__ __forceinline__ void one_by_one(const uint8_t* p, int there) {  // of any alignment of a channel
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < there) {
-                if constexpr (DT == OGC_F32) raw[i / 4][i % 4] = *(const uint32_t*)(p + 4 * i);
-                else raw[0][i / 2] |= (uint32_t) * (const uint16_t*)(p + 2 * i) << (i % 2 * 16);
-            }
+            for (int i = 0; i < 8; ++i)
+                if (i < there) {
+                    if constexpr (DT == OGC_F32) raw[i / 4][i % 4] = *(const uint32_t*)(p + 4 * i);
+                    else raw[0][i / 2] |= (uint32_t) * (const uint16_t*)(p + 2 * i) << (i % 2 * 16);
+                }
+        }
     }
     __device__ __forceinline__ void store(uint8_t* p, int there) const {
         if (there >= 8) {
