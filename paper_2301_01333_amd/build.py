@@ -234,7 +234,7 @@ def check_mx_loops(verbose: bool = True) -> None:
     import re
 
     kernels = 0
-    for source, many in (("ogc_mx.hip", 12), ("ogc_norm.hip", 37), ("ogc_mx_product.hip", 20), ("ogc_sample.hip", 8)):
+    for source, many in (("ogc_mx.hip", 12), ("ogc_norm.hip", 35), ("ogc_mx_product.hip", 20), ("ogc_sample.hip", 8)):
         text = _device_assembly(source)
         found = re.findall(r"\.name:\s+(\w*ogc_\w*kernel\w+)\s*\n\s+\.private_segment_fixed_size:\s+(\d+)", text)
         if len(found) != many or any(int(scratch) for _, scratch in found):

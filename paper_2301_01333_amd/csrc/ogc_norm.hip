@@ -3,8 +3,9 @@
 // Rows are read once, kept in registers, and written twice (the sum and its norm): the kernel is bound by memory, or by its launch.  A
 // lane holds N runs of eight channels.  In its own type a workgroup has one row; in a microscaled format it has eight, eight lanes of a
 // wavefront each, because the codes of eight rows are 128 bytes side by side in the matrix, and a wavefront's four runs of a row
-// are a block of 256 channels, whose four scales are one word.  Where that leaves compute units without work it has two rows, 32 lanes
-// each, whose runs are such a block.  Rows that do not fit the registers (N = 0) are read a second time for the norm.
+// are a block of 256 channels, whose four scales are one word.  Where that leaves compute units without work, or rows are long, it has two rows, 32 lanes
+// each, whose runs are such a block.  Many short rows are eight of a workgroup in any type.  Rows that do not fit the registers (N = 0) are read a second
+// time for the norm.
 // 8192 x 4096 in bf16 with a residual: in its own type 49 us (268 MB, 5.5 TB/s), to 8 bits 57 (236 MB, 4.1: the reads of eight rows and the codes' 128 bytes
 // cost what they save).  Many wavefronts with few runs each: eight runs a lane 56 and 63; tried for 8 bits and no better: rows read a kilobyte at
 // a time and turned in LDS (62).
@@ -157,21 +158,27 @@ template <int DT, int OUT, int ROWS> void launch(const NormArgs& a, hipStream_t 
             return;
         }
     }
-    if (runs <= 4) {
+    constexpr bool EIGHT = DT == OGC_BF16 && !(ROWS == 8 && OUT == OGC_NORM_SAME);  // (in fp32 they would not fit the registers)
+    if (runs <= 4 || (ROWS == 8 && !EIGHT)) {
         hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, ROWS, 4>), g, t, 0, st, a);
         return;
     }
-    if constexpr (DT == OGC_BF16) {  // (in fp32 they would not fit the registers)
-        if (runs <= 8) {
+    if constexpr (EIGHT) {
+        if (runs <= 8 || ROWS == 8) {
             hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, ROWS, 8>), g, t, 0, st, a);
             return;
         }
     }
-    hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, ROWS, 0>), g, t, 0, st, a);
+    if constexpr (ROWS != 8) hipLaunchKernelGGL((ogc_norm_kernel<DT, OUT, ROWS, 0>), g, t, 0, st, a);  // (eight rows are taken where they fit: see below)
 }
 template <int DT> void launch(int out, const NormArgs& a, hipStream_t s) {
-    const bool few = a.rows < 8 * 256;  // (eight rows each would leave compute units without work: 64 x 8192 in bf16 to 8 bits 5.7 us, eight rows each 12.5)
-    if (out == OGC_NORM_SAME) launch<DT, OGC_NORM_SAME, 1>(a, s);
+    // Two rows each or eight, us, of inputs from memory: bf16 to 8 bits 64 x 8192 5.7 / 12.5, 4097 x 4096 29.7 / 30.9, 5000 x 4096 35.5 / 34.1, 8192 x 4096 52.6 / 50.3, 32000 x
+    // 4096 241 / 175; to 4 bits 5000 x 4096 30.4 / 32.6, 8192 x 4096 46.2 / 48.4, 32000 x 4096 179 / 161; fp32 to 8 bits 5000 x 4096 55.6 / 63.7, 8192 x 4096 98 / 102,
+    // 32000 x 4096 384 / 341.  Rows that eight of a workgroup cannot hold in registers: bf16 3000 x 11000 45 / 65, fp32 3000 x 11000 106 / 137.
+    const bool few = a.rows <= (DT == OGC_F32 || out == OGC_NORM_MX4 ? 8192 : 4096) || a.padded > (DT == OGC_F32 ? 4096 : 8192);
+    // Many short rows, eight each or one: bf16 30000 x 100 10.0 / 23.0, 30000 x 256 11.7 / 14.7, 3000 x 100 6.2 / 5.2, 30000 x 512 19.1 / 20.2.
+    const bool short_rows = a.rows >= 8192 && a.padded == MX_BLOCK;
+    if (out == OGC_NORM_SAME) short_rows ? launch<DT, OGC_NORM_SAME, 8>(a, s) : launch<DT, OGC_NORM_SAME, 1>(a, s);
     else if (out == OGC_NORM_MX4) few ? launch<DT, OGC_NORM_MX4, 2>(a, s) : launch<DT, OGC_NORM_MX4, 8>(a, s);
     else few ? launch<DT, OGC_NORM_MX8, 2>(a, s) : launch<DT, OGC_NORM_MX8, 8>(a, s);
 }

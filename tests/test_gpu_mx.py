@@ -305,7 +305,9 @@ def test_norm_shapes(dtype, out, n, c):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("out,n,c", [("same", 2100, 100), ("same", 1500, 700), ("same", 1100, 4104), ("same", 1030, 9000), ("mx8", 8200, 300), ("mx8", 8211, 2048), ("mx4", 8193, 2304),
-                                      ("mx8", 2049, 100), ("mx4", 2051, 513), ("mx8", 2055, 1030), ("mx8", 2100, 4096), ("mx4", 2049, 4100), ("mx8", 2052, 5000)])
+                                      ("mx8", 2049, 100), ("mx4", 2051, 513), ("mx8", 2055, 1030), ("mx8", 2100, 4096), ("mx4", 2049, 4100), ("mx8", 2052, 5000),
+                                      ("mx8", 4100, 100), ("mx4", 4099, 513), ("mx8", 4111, 1030), ("mx8", 4097, 4096), ("mx4", 4097, 4100), ("mx8", 4098, 8192), ("mx8", 4099, 8200),
+                                      ("mx4", 8193, 100), ("mx4", 8209, 513), ("mx8", 8195, 1030), ("same", 8195, 100), ("same", 8193, 256), ("same", 8200, 7), ("same", 8192, 257)])
 def test_norm_of_many_rows(dtype, out, n, c):
     """Fewer wavefronts a row."""
     run_norm(dtype, n, c, out, True)
