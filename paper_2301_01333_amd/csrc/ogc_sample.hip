@@ -676,7 +676,7 @@ SAMPLE_DEV Result choose(Chosen& sh, int n, int vocab, const Weights& weights, f
     return found;
 }
 
-// How many of the first n sorted tokens are kept by top-p and min-p; `before`: the weight ahead of them.
+// How many of the first n sorted tokens are kept by top-p and min-p; `before`: the weight ahead of them; `goal`: top-p's, or 0: its share of these tokens' weight.
 template <int EACH> SAMPLE_DEV int kept_of(Chosen& sh, int n, const Weights& weights, const Limits& l, uint64_t before, uint64_t goal) {  // EACH: tokens of a thread
     if (threadIdx.x == 0) sh.found = n;
     uint64_t w[EACH], own = 0;
@@ -689,6 +689,7 @@ template <int EACH> SAMPLE_DEV int kept_of(Chosen& sh, int n, const Weights& wei
         own += w[e];
     }
     uint64_t all, run = before + sum_before(own, sh.part, all);
+    if (goal == 0) goal = goal_of(l.p, all);
     int mine = n;
 #pragma unroll
     for (int e = 0; e < EACH; ++e) {
@@ -741,10 +742,7 @@ template <int DT> SAMPLE_DEV bool by_top_k(const SampleArgs& a, Chosen& sh, cons
     if (n > MOST) return false;
     sort_by_logit<DT>(sh, n, a.vocab, min(low, key_of(logit_of(low))), key_of((float)weights.largest));
     n = min(n, l.k);
-    if (l.top_p || l.min_p) {
-        sum_before((int)threadIdx.x < n ? weights.of(key_in(sh.tokens[threadIdx.x])) : 0, sh.part, all);
-        n = kept_of<1>(sh, n, weights, l, 0, goal_of(l.p, all));
-    }
+    if (l.top_p || l.min_p) n = kept_of<1>(sh, n, weights, l, 0, 0);
     found = choose(sh, n, a.vocab, weights, u);
     return true;
 }
