@@ -357,7 +357,7 @@ template <int DT, int RUNS> __global__ __launch_bounds__(SCAN_THREADS) void ogc_
     const bool infinite = __builtin_amdgcn_readfirstlane(top == INFINITY);
     uint64_t sum = 0;
 #pragma unroll 1
-    for (int i = 0; i < RUNS; ++i) {  // (one after the other through x[0]: with all of them unrolled the code takes longer to come than the exponentials)
+    for (int i = 0; i < RUNS; ++i) {  // (one after the other through x[0]: eight exponentials side by side keep the pipe busy)
         uint64_t w[8];
         if (infinite) {
 #pragma unroll
@@ -868,8 +868,8 @@ template <int DT> SAMPLE_DEV bool by_parts(const SampleArgs& a, Chosen& sh, cons
     return true;
 }
 
-// ---- the choice, a workgroup for each row.  Bound by the latency of its steps (32000 bf16 logits with all limits 13 us: collecting 4, sorting 2, what top-p and min-p
-// keep 3, the choice 2), for long flat rows by a compute unit's way through their chunks (64 x 128000, top-p 30.8 us, 11 of them collecting).
+// ---- the choice, a workgroup for each row.  Bound by the latency of its steps (32000 bf16 logits with all limits 12.5 us: the limit of top-k 2, collecting 4, sorting 2,
+// what top-p and min-p keep 2, the choice 2), for long flat rows by a compute unit's way through their chunks (64 x 128000, top-p 30.8 us, 11 of them collecting).
 template <int DT> __global__ __launch_bounds__(THREADS) void ogc_sample_kernel(SampleArgs a) {
     __shared__ RowShared shared;
     Chosen& sh = shared.chosen;
