@@ -18,7 +18,7 @@
  *
  * Other tensors are DEVICE pointers to rows of contiguous channels, a stride apart (in elements; a multiple of 16 bytes; bases 16-byte aligned).
  * Rows that are read may overlap (a stride of 0 is the same row again), rows that are written must not.
- * Types: OGC_F32 and OGC_BF16.  Sums and norms are held in 32 bits; results are rounded once, to nearest even.
+ * Types: OGC_F32 and OGC_BF16.  Sums are held in 32 bits (the norm's in 64); results are rounded once, to nearest even.
  *
  * Every call is asynchronous on `stream` (a hipStream_t, NULL = the default stream) and may be captured into a graph; the library
  * allocates nothing and keeps nothing between calls.  Errors are return codes (ogc_status of ogc_mlp.h), found before any
@@ -42,14 +42,13 @@ ogc_status ogc_mx_bytes(int32_t format, int32_t rows, int32_t channels, size_t* 
 /* ---- the residual's addition with the root-mean-square norm ----------------------------------------------------------------------
  * For every row:   s = x + residual, rounded to the type (no residual: s = x)
  *                  y = s * rsqrt(mean_c(s[c]^2) + eps) * weight[c]
- * s is kept as the next residual.  Squares of eight channels are added up in fp32, these sums in 64 bits (magnitudes from 2^62 on may make a sum infinite,
- * and y zeros).  OGC_NORM_SAME: y in the type of x; OGC_NORM_MX4, OGC_NORM_MX8: y as a microscaled matrix, quantized from its
+ * s is kept as the next residual.  Squares and their sum are held in 64 bits, so that rows of all numbers have their norm; the factor is rounded to fp32.  OGC_NORM_SAME: y in the type of x; OGC_NORM_MX4, OGC_NORM_MX8: y as a microscaled matrix, quantized from its
  * fp32 values as by ogc_mx_write. */
 typedef enum { OGC_NORM_SAME = 0, OGC_NORM_MX4 = 1, OGC_NORM_MX8 = 2 } ogc_norm_out;
 
 typedef struct ogc_norm_desc {
     int32_t dtype;
-    int32_t rows, channels;     /* rows >= 0; channels > 0, at most 2^20 */
+    int32_t rows, channels;     /* rows >= 0, below 2^22; channels > 0, at most 2^20 */
     int32_t out;                /* ogc_norm_out */
     float eps;                  /* >= 0, finite */
     int64_t x_stride, residual_stride, sum_stride, y_stride; /* the residual's and the sum's: 0 without one; y's: OGC_NORM_SAME */
@@ -71,7 +70,7 @@ typedef enum { OGC_GATE_NONE = 0, OGC_GATE_SILU = 1 } ogc_gate;
 typedef struct ogc_mx_rows {
     int32_t dtype;
     int32_t format;             /* ogc_mx_format */
-    int32_t rows, channels;     /* rows >= 0; channels > 0, at most 2^20 */
+    int32_t rows, channels;     /* rows >= 0; channels > 0, at most 2^20; (rows / 32) * (channels / 256), rounded up, below 2^24 */
     int32_t gate;               /* ogc_gate; ogc_mx_read: OGC_GATE_NONE */
     int64_t stride;             /* of the rows of x or y */
 } ogc_mx_rows;

@@ -7,7 +7,8 @@
 // each, whose runs are such a block.  Many short rows are eight of a workgroup in any type.  Rows that do not fit the registers (N = 0) are read a second
 // time for the norm.
 // 8192 x 4096 in bf16 with a residual: in its own type 49 us (268 MB, 5.5 TB/s), to 8 bits 57 (236 MB, 4.1: the reads of eight rows and the codes' 128 bytes
-// cost what they save).  Many wavefronts with few runs each: eight runs a lane 56 and 63; tried for 8 bits and no better: rows read a kilobyte at
+// cost what they save).  Squares in 64 bits cost nothing there (50 us each of inputs from memory, as with sums
+// of eight in fp32), and 6 of 65 us for 3000 x 11000.  Many wavefronts with few runs each: eight runs a lane 56 and 63; tried for 8 bits and no better: rows read a kilobyte at
 // a time and turned in LDS (62).
 #include "ogc_mx_rows.h"
 
@@ -49,7 +50,7 @@ template <int DT, int OUT, int ROWS, int N> __global__ __launch_bounds__(64 * NO
     const int runs = (limit + SPAN * waves - 1) / (SPAN * waves) * RUNS;
 
     MxEight<DT> held[N > 0 ? N : 1];
-    double square = 0.0;  // eight squares are added up in fp32, these sums in 64 bits: the factor of a row is the rounded one, whatever its length
+    double square = 0.0;  // in 64 bits: squares of all numbers are some there, and the factor of a row is the rounded one, whatever its length
     const auto take = [&](MxEight<DT>& s, const MxEight<DT>& more, int c) {
         const int there = on ? a.channels - c : 0;
         float v[8];
@@ -59,10 +60,8 @@ template <int DT, int OUT, int ROWS, int N> __global__ __launch_bounds__(64 * NO
             s.set(v);  // (rounded: the norm is the norm of what the next layer adds to)
             if (there > 0) s.store(sum + (int64_t)c * E, there);
         }
-        float eight = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) eight = __builtin_fmaf(s.get(i), s.get(i), eight);
-        square += (double)eight;
+        for (int i = 0; i < 8; ++i) square = __builtin_fma((double)s.get(i), (double)s.get(i), square);
     };
     if constexpr (N > 0) {
         MxEight<DT> more[N];
@@ -93,7 +92,11 @@ template <int DT, int OUT, int ROWS, int N> __global__ __launch_bounds__(64 * NO
         square = 0.0;
         for (int w = 0; w < waves; ++w) square += part[w][lane / LANES];
     }
-    const float f = (float)(1.0 / __builtin_sqrt(square * a.inv + (double)a.eps));
+    // The factor of the largest rows is no normal fp32 number, and that of the smallest ones is beyond all of them: there a value takes a part of it first, a power of two, without rounding (or what is
+    // lost is below the smallest result).
+    const double root = __builtin_sqrt(square * a.inv + (double)a.eps);
+    const float power = root > 0x1p100 ? 0x1p-64f : root < 0x1p-100 ? 0x1p64f : 1.0f;
+    const float f = (float)(1.0 / (root * (double)power));
 
     const auto give = [&](const MxEight<DT>& s, int c, uint32_t& scales, int i) {
         const int there = on ? a.channels - c : 0;
@@ -101,10 +104,10 @@ template <int DT, int OUT, int ROWS, int N> __global__ __launch_bounds__(64 * NO
         if (there >= 8) {
             const mx_v4f w0 = *(const mx_v4f*)(a.weight + c), w1 = *(const mx_v4f*)(a.weight + c + 4);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = s.get(k) * f * (k < 4 ? w0[k % 4] : w1[k % 4]);
+            for (int k = 0; k < 8; ++k) v[k] = s.get(k) * power * f * (k < 4 ? w0[k % 4] : w1[k % 4]);
         } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = k < there ? s.get(k) * f * a.weight[c + k] : 0.0f;
+            for (int k = 0; k < 8; ++k) v[k] = k < there ? s.get(k) * power * f * a.weight[c + k] : 0.0f;
         }
         if constexpr (OUT == OGC_NORM_SAME) {
             MxEight<DT> y;
