@@ -2,8 +2,8 @@
 //
 // Both kernels move every value once and are bound by memory, or by their launch.  A workgroup has 256 channels of 32 rows, a wavefront eight
 // of the rows, a lane eight channels of each of four runs of 64: rows are read 128 bytes (fp32: 256) at a time, the codes
-// of eight rows leave as 128 bytes side by side, and a lane's four scales of a row are one word of the matrix.  bf16, 4096 x 8192: a gated pair to 8 bits 36 us
-// (169 MB, 4.7 TB/s), back 16 us (101 MB, 6.2 TB/s); fp32, 2001 x 4500: to 4 bits 8.6 us (41 MB, 4.8 TB/s).
+// of eight rows leave as 128 bytes side by side, and a lane's four scales of a row are one word of the matrix.  bf16, 4096 x 8192: a gated pair to 8 bits 37 us
+// (169 MB, 4.5 TB/s; 36 without the look for gates at fp32's ends), back 16 us (101 MB, 6.2 TB/s); fp32, 2001 x 4500: to 4 bits 8.6 us (41 MB, 4.8 TB/s).
 #include "ogc_mx_rows.h"
 
 #include <math.h>
@@ -18,14 +18,22 @@ struct RowsArgs {
     int rows, channels, padded, blocks;  // blocks: of 256 channels
 };
 
-// a * b / (1 + exp(-a)).  exp(-|a|) neither overflows nor loses what the product of |a| and log2(e) is rounded by (from |a| = 104 on it is 0 in fp32, and from
-// 2.3e38 on that product would be an infinity).
+// a * b / (1 + exp(-a)) for a from -80 on, but 0 < |a| < 2^-125: there neither exp(-|a|) nor its product with a is below the normal numbers, which the instruction for powers of two does not give,
+// and only the last product is rounded to what is there.  exp(-|a|) does not lose what the product of |a| and log2(e) is rounded by (and is 0 from some 87 on).
 MX_DEV float gated(float a, float b) {
     const float m = __builtin_fmaxf(-__builtin_fabsf(a), -128.0f), hi = m * 1.44269502162933349609f;
     const float lo = __builtin_fmaf(m, 1.44269502162933349609f, -hi) + m * 1.92596299112661746887e-8f;
     float t = __builtin_amdgcn_exp2f(hi);
     t = __builtin_fmaf(t, lo * 0.69314718055994530942f, t);
     return a * ((a < 0.0f ? t : 1.0f) * __builtin_amdgcn_rcpf(1.0f + t)) * b;  // (the reciprocal is off by 2^-23)
+}
+// The same for every a, in 64 bits: b may be as large as exp(-|a|) is small.  (e^-512 of any two numbers is none.)
+MX_DEV float gated_far(float a, float b) {
+    const float m = __builtin_fmaxf(-__builtin_fabsf(a), -512.0f), hi = m * 1.44269502162933349609f, n = __builtin_rintf(hi);
+    const float lo = __builtin_fmaf(m, 1.44269502162933349609f, -hi) + m * 1.92596299112661746887e-8f;
+    const float f = __builtin_amdgcn_exp2f(hi - n);
+    const double t = __builtin_amdgcn_ldexp((double)__builtin_fmaf(f, lo * 0.69314718055994530942f, f), (int)n);
+    return (float)((double)a * (a < 0.0f ? t : 1.0) / (1.0 + t) * (double)b);
 }
 
 template <int DT, int FORMAT, int GATE> __global__ __launch_bounds__(256) void ogc_mx_write_kernel(RowsArgs a) {
@@ -50,6 +58,28 @@ template <int DT, int FORMAT, int GATE> __global__ __launch_bounds__(256) void o
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = GATE ? gated(x[s].get(i), y[GATE ? s : 0].get(i)) : x[s].get(i);
+        if constexpr (GATE) {
+            float least = 0.0f;
+            uint32_t nearest = 0xffffffffu;  // to 0, which is none itself
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                least = __builtin_fminf(least, x[s].get(i));
+                nearest = min(nearest, (__builtin_bit_cast(uint32_t, x[s].get(i)) & 0x7fffffffu) - 1);
+            }
+            const bool far = (least < -80.0f) | (nearest < 0x00ffffffu);  // (2^-125 is 0x01000000)
+            if (__builtin_expect(far, 0)) {
+                MxEight<DT> p = x[s], q = y[GATE ? s : 0];
+#pragma unroll 1
+                for (int i = 0; i < 8; ++i) {  // (a loop, of a value at a time: code that is hardly ever run shall not be in the way of the other)
+                    const float far_one = gated_far(p.get(0), q.get(0));
+#pragma unroll
+                    for (int k = 0; k < 7; ++k) v[k] = v[k + 1];
+                    v[7] = far_one;
+                    p.next();
+                    q.next();
+                }
+            }
+        }
         uint32_t e;
         code[s] = mx_quantized<FORMAT>(v, e);
         scales |= e << (8 * s);

@@ -59,6 +59,16 @@ template <int DT> struct MxEight {
         if constexpr (DT == OGC_F32) return __builtin_bit_cast(float, (uint32_t)raw[i / 4][i % 4]);
         else return __builtin_bit_cast(float, i & 1 ? (uint32_t)raw[0][i / 2] & 0xffff0000u : (uint32_t)raw[0][i / 2] << 16);
     }
+    __device__ __forceinline__ void next() {  // channel 1 in the place of channel 0, and so on
+        if constexpr (DT == OGC_F32) {
+            const uint32_t first = raw[0][0];
+            raw[0] = (mx_v4u){raw[0][1], raw[0][2], raw[0][3], raw[1][0]};
+            raw[1] = (mx_v4u){raw[1][1], raw[1][2], raw[1][3], first};
+        } else {
+            const mx_v4u t = raw[0];
+            raw[0] = (mx_v4u){t[0] >> 16 | t[1] << 16, t[1] >> 16 | t[2] << 16, t[2] >> 16 | t[3] << 16, t[3] >> 16 | t[0] << 16};
+        }
+    }
     __device__ __forceinline__ void set(const float (&x)[8]) {  // bf16: rounded to nearest even
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
