@@ -194,7 +194,7 @@ class DecoderLayer:
 
 class TokenChoice:
     """Chooses a token of each of `rows` rows of `vocab` logits: temperature, top-k, top-p and min-p as tensors [rows] (None: 1, and no limit).
-    Calls share a workspace: they belong on one stream, or graphs that do not run at the same time."""
+    Every call has a workspace of its own, from PyTorch's pool of its stream or graph, so that calls on several streams, and captured ones, may run at the same time."""
 
     def __init__(self, rows: int, vocab: int, dtype, temperature=None, top_k=None, top_p=None, min_p=None):
         import torch
@@ -204,8 +204,9 @@ class TokenChoice:
             if t is not None and (t.dtype != kind or tuple(t.shape) != (rows,) or not t.is_contiguous() or not on_this_gpu(t)):
                 raise ValueError("%s of %s %s on %s, not %s [%d], contiguous, on the GPU" % (what, t.dtype, list(t.shape), t.device, kind, rows))
         self.rows, self.vocab, self.dtype, self.limits = rows, vocab, dtype, (temperature, top_k, top_p, min_p)
+        self.device = torch.device("cuda", torch.cuda.current_device())
         # (for rows of any stride)
-        self.workspace = torch.empty(max(16, binding.ogc_sample_workspace_bytes(binding.sample_desc(_types()[dtype], rows, vocab, vocab))), dtype=torch.uint8, device="cuda")
+        self.workspace_bytes = max(16, binding.ogc_sample_workspace_bytes(binding.sample_desc(_types()[dtype], rows, vocab, vocab)))
 
     def __call__(self, logits, uniform):
         """(tokens int32 [rows], their log-probabilities float32 [rows]); uniform: float32 [rows], random numbers from 0 to 1."""
@@ -213,15 +214,16 @@ class TokenChoice:
 
         if tuple(logits.shape) != (self.rows, self.vocab) or logits.dtype != self.dtype or not on_this_gpu(logits) or (self.vocab > 1 and logits.stride(1) != 1):
             raise ValueError("logits of %s %s on %s, not %s [%d, %d], next to each other, on the GPU" % (logits.dtype, list(logits.shape), logits.device, self.dtype, self.rows, self.vocab))
-        if self.workspace.device != logits.device:
-            raise ValueError("logits on %s, the workspace on %s" % (logits.device, self.workspace.device))
+        if self.device != logits.device:
+            raise ValueError("logits on %s, the limits on %s" % (logits.device, self.device))
         if uniform.dtype != torch.float32 or tuple(uniform.shape) != (self.rows,) or not uniform.is_contiguous() or uniform.device != logits.device:
             raise ValueError("uniform of %s %s on %s, not float32 [%d], contiguous, on %s" % (uniform.dtype, list(uniform.shape), uniform.device, self.rows, logits.device))
         tokens = torch.empty(self.rows, dtype=torch.int32, device="cuda")
         logs = torch.empty(self.rows, dtype=torch.float32, device="cuda")
+        space = torch.empty(self.workspace_bytes, dtype=torch.uint8, device="cuda")
         desc = binding.sample_desc(_types()[self.dtype], self.rows, self.vocab, logits.stride(0) if self.rows > 1 else self.vocab)
         binding.ogc_sample_run(desc, logits.data_ptr(), *(0 if t is None else t.data_ptr() for t in self.limits), uniform.data_ptr(), tokens.data_ptr(), logs.data_ptr(),
-                               self.workspace.data_ptr(), _stream())
+                               space.data_ptr(), _stream())
         return tokens, logs
 
 
