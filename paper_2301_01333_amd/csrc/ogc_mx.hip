@@ -2,8 +2,8 @@
 //
 // Both kernels move every value once and are bound by memory, or by their launch.  A workgroup has 256 channels of 32 rows, a wavefront eight
 // of the rows, a lane eight channels of each of four runs of 64: rows are read 128 bytes (fp32: 256) at a time, the codes
-// of eight rows leave as 128 bytes side by side, and a lane's four scales of a row are one word of the matrix.  bf16, 4096 x 8192: a gated pair to 8 bits 37 us
-// (169 MB, 4.5 TB/s; 36 without the look for gates at fp32's ends), back 16 us (101 MB, 6.2 TB/s); fp32, 2001 x 4500: to 4 bits 8.6 us (41 MB, 4.8 TB/s).
+// of eight rows leave as 128 bytes side by side, and a lane's four scales of a row are one word of the matrix.  bf16, 4096 x 8192: a gated pair to 8 bits 36 us
+// (169 MB, 4.7 TB/s), back 16 us (101 MB, 6.2 TB/s); fp32, 2001 x 4500: to 4 bits 8.6 us (41 MB, 4.8 TB/s).
 #include "ogc_mx_rows.h"
 
 #include <math.h>
@@ -59,14 +59,15 @@ template <int DT, int FORMAT, int GATE> __global__ __launch_bounds__(256) void o
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = GATE ? gated(x[s].get(i), y[GATE ? s : 0].get(i)) : x[s].get(i);
         if constexpr (GATE) {
-            float least = 0.0f;
-            uint32_t nearest = 0xffffffffu;  // to 0, which is none itself
+            // (of the bits: negative numbers are above the others, and the larger the further from 0)
+            uint32_t most = 0, nearest = 0xffffffffu;  // nearest to 0, which is none itself
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                least = __builtin_fminf(least, x[s].get(i));
-                nearest = min(nearest, (__builtin_bit_cast(uint32_t, x[s].get(i)) & 0x7fffffffu) - 1);
+                const uint32_t bits = __builtin_bit_cast(uint32_t, x[s].get(i));
+                most = max(most, bits);
+                if constexpr (DT == OGC_F32) nearest = min(nearest, (bits & 0x7fffffffu) - 1);  // (bf16: a half of the smallest is a number of fp32)
             }
-            const bool far = (least < -80.0f) | (nearest < 0x00ffffffu);  // (2^-125 is 0x01000000)
+            const bool far = (most > 0xc2a00000u) | (nearest < 0x00ffffffu);  // -80; 2^-125 is 0x01000000
             if (__builtin_expect(far, 0)) {
                 MxEight<DT> p = x[s], q = y[GATE ? s : 0];
 #pragma unroll 1
