@@ -23,7 +23,7 @@
  * Every call is asynchronous on `stream` (a hipStream_t, NULL = the default stream) and may be captured into a graph; the library
  * allocates nothing and keeps nothing between calls.  Errors are return codes (ogc_status of ogc_mlp.h), found before any
  * launch: OGC_ERR_INVALID_ARG (NULL, an unknown enum, a scalar out of range), OGC_ERR_SHAPE (sizes), OGC_ERR_UNSUPPORTED (types),
- * OGC_ERR_ALIGNMENT (strides, pointers), OGC_ERR_WORKSPACE (none where one is needed), OGC_ERR_DEVICE (a launch failed).  Calls without rows do nothing.
+ * OGC_ERR_ALIGNMENT (strides, pointers), OGC_ERR_DEVICE (a launch failed).  Calls without rows do nothing.
  */
 #ifndef OGC_MX_H
 #define OGC_MX_H
@@ -93,10 +93,9 @@ typedef struct ogc_mx_product_desc {
 } ogc_mx_product_desc;
 
 ogc_status ogc_mx_product_validate(const ogc_mx_product_desc* desc);
-/* Bytes that a call needs at `workspace` (0: none). */
+/* Bytes that a call needs at `workspace`: 0, for every description.  (The product has the form of the calls that do need one.) */
 ogc_status ogc_mx_product_workspace_bytes(const ogc_mx_product_desc* desc, size_t* bytes);
-/* bias: fp32 [n], 4-byte aligned, unless has_bias is 0.  y must not overlap the inputs.  workspace: 16-byte aligned, contents do not matter; calls that
- * may run at the same time need different ones. */
+/* bias: fp32 [n], 4-byte aligned, unless has_bias is 0.  y must not overlap the inputs.  workspace: not looked at, and may be NULL. */
 ogc_status ogc_mx_product_run(const ogc_mx_product_desc* desc, const void* x, const void* x_scales, const void* w, const void* w_scales,
                               const float* bias, void* y, void* workspace, void* stream);
 /* Name of the kernel that ogc_mx_product_run launches for this description, as a kernel trace prints it (static storage), or NULL. */

@@ -136,8 +136,6 @@ class Projection:
         self.bias = bias
 
     def __call__(self, x: MxMatrix, dtype):
-        import torch
-
         if x.channels != self.weight.channels:
             raise ValueError("rows of %d channels for weights of %d" % (x.channels, self.weight.channels))
         kind = _type(dtype, "a result")
@@ -146,10 +144,8 @@ class Projection:
         n = self.weight.rows
         y = _rows(x.rows, n, dtype)
         desc = binding.mx_product_desc(kind, FORMATS[x.fmt], binding.OGC_MX4, x.rows, n, x.channels, int(self.bias is not None), _stride(y))
-        need = binding.ogc_mx_product_workspace_bytes(desc)
-        space = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
         binding.ogc_mx_product_run(desc, x.codes.data_ptr(), x.scales.data_ptr(), self.weight.codes.data_ptr(), self.weight.scales.data_ptr(),
-                                   self.bias.data_ptr() if self.bias is not None else 0, y.data_ptr(), space.data_ptr() if need else 0, _stream())
+                                   self.bias.data_ptr() if self.bias is not None else 0, y.data_ptr(), 0, _stream())
         return y
 
 
@@ -158,7 +154,8 @@ class DecoderLayer:
     nothing), and returns the same for the next layer: each sum meets its norm in one pass.
 
     attention: a DecoderAttention of the layer's heads.  Weights: qkv [heads * head_dim, channels] of queries, keys and values, out [channels, query heads *
-    head_dim], gate_up [2 * hidden, channels], down [channels, hidden]; norms fp32 [channels].  rows: the format of the rows between them."""
+    head_dim], gate_up [2 * hidden, channels], down [channels, hidden]; norms fp32 [channels].  rows: the format of the rows between them.  A layer's calls belong on one stream, one after
+    the other, or in graphs that are replayed so: they share the attention's cache and its workspace."""
 
     def __init__(self, attention: DecoderAttention, qkv, out, gate_up, down, norm_attention, norm_feed_forward, eps: float = 1e-6, rows: str = "mx8"):
         a, c = attention, out.shape[0]
