@@ -10,7 +10,7 @@
 // ones have landed.
 //
 // Bound by power: 4096 x 8192 x 8192 of 4 bits 125 to 129 us (4.3 PFLOP/s) at 1.82 GHz, at which the matrix pipe is busy 56 % of the cycles, LDS 26, with no
-// conflicts; with 8-bit rows 192 us (2.9).  A stage takes 0.83 us (5.2 PFLOP/s; 8-bit rows 1.36, 3.2), the instructions alone reach 5.6 (3.5) on random data in
+// conflicts; with 8-bit rows, bf16 results, 192 us (2.9).  A stage takes 0.83 us (5.2 PFLOP/s; 8-bit rows 1.36, 3.2), the instructions alone reach 5.6 (3.5) on random data in
 // registers.  256 x 256 with eight wavefronts of 128 x 64 each pulls half the bytes of 128 x 128 through LDS, whose four wavefronts have 64 x 64.
 #ifndef OGC_MX_TILE_H
 #define OGC_MX_TILE_H
