@@ -82,8 +82,8 @@ ogc_status ogc_mx_read(const ogc_mx_rows* rows, const void* codes, const void* s
 
 /* ---- product ---------------------------------------------------------------------------------------------------------------------
  * y[i][j] = sum_c x[i][c] w[j][c] + bias[j],  x [m][k] and w [n][k] microscaled matrices.  Products are exact; those of eight neighbouring channels are added without
- * loss, these sums in fp32, 8-bit rows as two sums each (codes below 2 and the others).  Only bf16 results of OGC_MX8 rows may have less, where ogc_mx_product_kernel_name names
- * tiles (calls of many rows): of eight products what is below 2^-14 of the largest one's power of two is dropped (measured: 4e-6 of a result of random rows). */
+ * loss, these sums in fp32, 8-bit rows as two sums each (codes below 2 and the others).  Only bf16 results of OGC_MX8 rows may have less, where a call has many rows (ogc_mx_product_kernel_name: not
+ * ogc_mx_few_kernel<.., 1>): of eight products what is below 2^-14 of the largest one's power of two is dropped (measured: 4e-6 of a result of random rows). */
 typedef struct ogc_mx_product_desc {
     int32_t dtype;              /* of y */
     int32_t x_format, w_format; /* OGC_MX4 or OGC_MX8; OGC_MX4 */

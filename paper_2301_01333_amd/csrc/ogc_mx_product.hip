@@ -54,9 +54,9 @@ template <int XF, int I> MX_DEV v16f instruction(const Operand<OGC_MX4>& w, cons
 //
 // The instruction adds the products of eight neighbouring channels on their own, and drops what of them is below 2^-14 of the largest one's power of two; with the others and with c
 // it adds them up in fp32 (measured).  Products of E2M1 codes span 8 bits, all of which stay.  With E4M3 codes they span 22, but 15 where |x| is from 2 on and 14
-// where it is below 2: WHOLE, rows of 8 bits are multiplied in these two parts, and their sums are fp32 sums too.
-template <int XF, int I, bool WHOLE> MX_DEV v16f product(const Operand<OGC_MX4>& w, const Operand<XF>& x, v16f c, uint32_t ws, uint32_t xs) {
-    if constexpr (XF == OGC_MX8 && WHOLE) {
+// where it is below 2: with PARTS rows of 8 bits are multiplied in these two, and their sums are fp32 sums too.
+template <int XF, int I, bool PARTS> MX_DEV v16f product(const Operand<OGC_MX4>& w, const Operand<XF>& x, v16f c, uint32_t ws, uint32_t xs) {
+    if constexpr (XF == OGC_MX8 && PARTS) {
         Operand<OGC_MX8> low, high;
         split(x, low, high);
         return instruction<XF, I>(w, high, instruction<XF, I>(w, low, c, ws, xs), ws, xs);
@@ -91,10 +91,11 @@ constexpr int FEW_WAVES = 4;
 // A workgroup has NB blocks of 32 weights and MB blocks of 32 rows; its wavefronts take the channels in turn, 256 at a time, straight from memory into registers
 // (nothing that one of them reads is read by another of them), and add up in LDS.  With 8-bit rows and operands from memory (sets that take turns over 600 MB), us: 32 x 32000 x 4096
 // 18.2 (3.9 TB/s), 16 x 4096 x 4096 6.7, 1 x 4096 x 14336 16.0: few rows are bound by memory and, where workgroups do not fill the chip, by the latency of a wavefront's
-// loads, which are all on their way at once.  (As the compiler would have them they take 6.1 where these take 4.4: 32 x 8192 x 4096 from the caches, 8-bit rows whole.)  More rows are bound by what a compute
-// unit's load path brings in, some 40 bytes a clock, and by the matrix instructions: 256 x 8192 x 4096 19.1.  Rows whole would take 17.4, 6.2, 14.8 and 15.8: most of the second instruction is in the shadow
-// of the loads.
+// loads, which are all on their way at once.  (As the compiler would have them: 6.1 for 4.4, 32 x 8192 x 4096 from the caches, rows whole.)  More rows are bound by what a compute
+// unit's load path brings in, some 40 bytes a clock (256 x 8192 x 4096 15.9).  Blocks of 32 rows have them in two parts: whole, these would take 17.4, 6.2 and 14.8.  Tried for the two parts and no
+// better: the next 256 channels' loads ahead of them (half as many wavefronts have room: 64 x 1024 x 8192 8.0, the same, 256 x 4096 x 4096 15.0 instead of 11.6).
 template <int DT, int XF, int NB, int MB> __global__ __launch_bounds__(64 * FEW_WAVES) void ogc_mx_few_kernel(ProductArgs a) {
+    constexpr bool PARTS = DT == OGC_F32 || MB == 1;  // (blocks of 64 rows wait for the matrix instructions; see the tiles)
     constexpr int PITCH = 36;  // floats of a row's 32 sums: the 16-byte pieces of eight rows are on distinct banks
     __shared__ __attribute__((aligned(16))) float sums[FEW_WAVES][32 * PITCH];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -145,10 +146,10 @@ template <int DT, int XF, int NB, int MB> __global__ __launch_bounds__(64 * FEW_
         for (int i = 0; i < NB; ++i)
 #pragma unroll
             for (int j = 0; j < MB; ++j) {
-                c[i][j] = product<XF, 0, true>(p[i][0], q[j][0], c[i][j], u[i], v[j]);
-                c[i][j] = product<XF, 1, true>(p[i][1], q[j][1], c[i][j], u[i], v[j]);
-                c[i][j] = product<XF, 2, true>(p[i][2], q[j][2], c[i][j], u[i], v[j]);
-                c[i][j] = product<XF, 3, true>(p[i][3], q[j][3], c[i][j], u[i], v[j]);
+                c[i][j] = product<XF, 0, PARTS>(p[i][0], q[j][0], c[i][j], u[i], v[j]);
+                c[i][j] = product<XF, 1, PARTS>(p[i][1], q[j][1], c[i][j], u[i], v[j]);
+                c[i][j] = product<XF, 2, PARTS>(p[i][2], q[j][2], c[i][j], u[i], v[j]);
+                c[i][j] = product<XF, 3, PARTS>(p[i][3], q[j][3], c[i][j], u[i], v[j]);
             }
     }
     const int row = threadIdx.x / 8, at = threadIdx.x % 8 * 4;
@@ -178,15 +179,15 @@ template <int DT, int XF, int NB, int MB> __global__ __launch_bounds__(64 * FEW_
 
 namespace {
 
-// Which kernel a call takes, the same for its launch and its name: the one that takes the least time by costs that are fitted to all five of them.  For 8-bit rows at 118 sizes (m 1 .. 8192, n 90 ..
-// 32000, k 64 .. 16384), bf16 results, operands from memory (sets that take turns over 600 MB): the choice is 0.5 % above the fastest in the mean, 25 % at most.  us, of wavefronts that share the
-// channels in blocks of 32 x 32 / 64 x 32 / 64 x 64, and of tiles of 128 x 128 / 256 x 256: 16 x 8192 x 4096 7.9 / 8.8 / 11.4 / 16.9 / 40; 128 x 8192 x 4096 14.9 / 12.5 / 13.0 / 17.5 / 41;
-// 256 x 8192 x 4096 25.9 / 19.6 / 19.1 / 18.0 / 39; 512 x 8192 x 4096 44 / 33 / 33 / 19.8 / 40; 1024 x 14336 x 4096 153 / 110 / 108 / 60 / 51.  (fp32 results, whose tiles take up to 1.8 times as long,
-// go by the same costs.)  For rows of 4 bits at 95 sizes, of the same operands each time, which stay in the caches: 0.6 % in the mean, 17 % at most.
+// Which kernel a call takes, the same for its launch and its name: the one that takes the least time by costs that are fitted to all five of them.  For 8-bit rows at 117 sizes (m 1 .. 8192, n 90 ..
+// 32000, k 64 .. 16000), bf16 results, operands from memory (sets that take turns over 600 MB): the choice is 0.3 % above the fastest in the mean, 7 % at most.  us, of wavefronts that share the
+// channels in blocks of 32 x 32 / 64 x 32 / 64 x 64, and of tiles of 128 x 128 / 256 x 256: 16 x 8192 x 4096 7.9 / 8.8 / 9.7 / 17.0 / 40; 128 x 8192 x 4096 14.9 / 12.7 / 11.0 / 17.5 / 41;
+// 256 x 8192 x 4096 25.6 / 19.3 / 15.9 / 17.8 / 39; 512 x 8192 x 4096 44 / 33 / 25 / 19.8 / 40; 1024 x 14336 x 4096 152 / 107 / 79 / 60 / 51.  (fp32 results go by the same costs; blocks of 64 x 64 take up to
+// 1.3 times as long for them, tiles 1.8 times.)  For rows of 4 bits at 95 sizes, of the same operands each time, which stay in the caches: 0.6 % in the mean, 17 % at most.
 // A wavefront's share of 256 channels takes its own time, or its part of what all workgroups have to pull in; the ones beyond 512 take turns, ends included.
 // Tiles of 256 x 256 have a compute unit to themselves, so that 256 of them take as long as one, and no product hides their first loads and last stores;
 // two of 128 x 128 share a compute unit, but pull twice the bytes through LDS (small / large, us: 4 bits 8192 x 8192 x 512 37.8 / 41.6, 4096 x 4096 x 2048
-// 24.7 / 23.2, 8192 x 8192 x 8192 285 / 242; 8-bit rows 4096 x 4096 x 512 19.3 / 16.7, 4096 x 8192 x 8192 216 / 194).
+// 24.7 / 23.2, 8192 x 8192 x 8192 285 / 242; 8-bit rows 4096 x 4096 x 512 19.4 / 18.0, 4096 x 8192 x 8192 216 / 194).
 enum { FEW_1, FEW_2, FEW_4, TILE_128, TILE_256 };
 constexpr int64_t MOST_SMALL = 0xfffff8, MOST_LARGE = 0x7ffff8;  // tiles of a launch of fewer than 2^32 threads, 256 and 512 a tile; multiples of eight
 int kernel_for(const ogc_mx_product_desc* d) {
@@ -199,12 +200,12 @@ int kernel_for(const ogc_mx_product_desc* d) {
         return start + share * std::max(own, part * (double)groups) + turn * (double)std::max<int64_t>(0, groups - 512);
     };
     const int64_t rest = small % 512;
-    const double of_rest = rest == 0 ? 0.0 : eight ? 5.1 + 1.1 * stages * (rest <= 128 ? 0.38 : rest <= 256 ? 0.37 : 1.0)
+    const double of_rest = rest == 0 ? 0.0 : eight ? 5.0 + 1.1 * stages * (rest <= 128 ? 0.40 : rest <= 256 ? 0.39 : 1.0)
                                                    : 4.7 + 0.68 * stages * (rest <= 128 ? 0.29 : rest <= 256 ? 0.40 : 1.0);
-    const double cost[5] = {eight ? few(count(32, 32), 3.5, 0.59, 0.003, 0.0005) : few(count(32, 32), 2.7, 0.24, 0.0013, 0.00044),
-                            eight ? few(count(64, 32), 4.0, 0.92, 0.0035, 0.0018) : few(count(64, 32), 3.5, 0.30, 0.0017, 0.0012),
-                            eight ? few(count(64, 64), 6.0, 1.7, 0.0059, 0.0048) : few(count(64, 64), 5.2, 0.43, 0.0026, 0.0023),
-                            (double)(small / 512) * (eight ? 5.2 + 0.89 * stages : 3.0 + 0.51 * stages) + of_rest,
+    const double cost[5] = {eight ? few(count(32, 32), 3.3, 0.71, 0.0030, 0.00054) : few(count(32, 32), 2.7, 0.24, 0.0013, 0.00044),
+                            eight ? few(count(64, 32), 3.8, 0.92, 0.0041, 0.0013) : few(count(64, 32), 3.5, 0.30, 0.0017, 0.0012),
+                            eight ? few(count(64, 64), 5.5, 1.1, 0.0047, 0.0048) : few(count(64, 64), 5.2, 0.43, 0.0026, 0.0023),
+                            (double)(small / 512) * (eight ? 5.6 + 0.86 * stages : 3.0 + 0.51 * stages) + of_rest,
                             (double)((count(256, 256) + 255) / 256) * (eight ? 11.0 + 1.2 * stages : 7.0 + 0.83 * stages)};
     const int first = count(32, 32) > MOST_SMALL ? TILE_128 : FEW_1;
     return (int)(std::min_element(cost + first, cost + 5) - cost);

@@ -50,7 +50,7 @@ template <int DT, int XF, int WN, int WM, int NB, int MB>
 __global__ __launch_bounds__(64 * WN * WM, NB * MB > 8 ? 1 : 2) void ogc_mx_tile_kernel(ProductArgs a) {
     typedef MxTile<XF, WN, WM, NB, MB> T;
     // 8-bit rows in two parts take 356 us instead of 194 (4096 x 8192 x 8192).  Whole, random rows lose 4e-6 of a result: bf16 results, which are rounded by 2^-8 of it, have them whole, fp32 results do not.
-    constexpr bool WHOLE = DT == OGC_F32;
+    constexpr bool PARTS = DT == OGC_F32;
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     const uint32_t lds = (uint32_t)(uintptr_t)(mx_lds_u8*)smem;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(64 * WN * WM, NB * MB > 8 ? 1 : 2) void ogc_mx_tile
         for (int j = 0; j < MB; ++j)
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
-                c[i][j] = product<XF, quarter, WHOLE>(p[f][i], q[f][j], c[i][j], sp[i], sq[j]);
+                c[i][j] = product<XF, quarter, PARTS>(p[f][i], q[f][j], c[i][j], sp[i], sq[j]);
                 between(j * NB + i);
             }
     };
